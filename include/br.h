@@ -298,6 +298,79 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
                      double *mu_rem);
 
 /*
+ * The paged caches of the decode workers.  (The paper leaves them to the engine; these entry points keep them in line with
+ * the requests that br_step places, lets grow and ends, without a trip to the host.)
+ *
+ * Each worker keeps its requests' keys and values in pool_blocks cache blocks of block_tokens tokens, numbered from 0.  Row b
+ * of its block table names the blocks of the request in slot b, in token order; the blocks that no request holds are the
+ * first n_free entries of its free list.  A new cache: n_blocks = 0, n_free = pool_blocks, free_list any order of the
+ * blocks (fewer entries keep blocks out of use, e.g. one for padding).
+ *
+ * All three calls read the tokens of each request from len [N][G][B]: len + step[i] with step [N], so that act_base and step
+ * of br_worker_state serve as they are after br_step, or len itself with step NULL; BR_EMPTY_SLOT and sums below 1 are free
+ * slots, sums beyond 2^31 - 1 count as that.  Device pointers aligned to their type; asynchronous on batch.stream, whose
+ * device must be current; batch.n_steps is not used.  BR_EINVAL for null or misaligned pointers, sizes outside the limits and
+ * (first_instance + n_instances) * G beyond 2^31 - 1; BR_ECUDA if the launch failed.  No context is needed and nothing
+ * allocated; calls on different rows may overlap, and all may be captured into graphs.
+ */
+#define BR_MAX_BLOCK_TOKENS (1 << 20)
+#define BR_MAX_TABLE_BLOCKS (1 << 22)
+#define BR_MAX_POOL_BLOCKS  (1 << 28)
+
+typedef struct {
+    int32_t  G, B;          /* workers per instance and slots per worker: 1 <= G <= BR_MAX_G, 1 <= B <= BR_MAX_B */
+    int32_t  block_tokens;  /* tokens per block                                                */
+    int32_t  pool_blocks;   /* blocks per worker                                               */
+    int32_t  table_blocks;  /* columns of a table row: the most blocks a request may hold      */
+    int32_t *table;         /* [N][G][B][table_blocks] block numbers; entries from n_blocks on are not used */
+    int32_t *n_blocks;      /* [N][G][B] blocks held                                           */
+    int32_t *free_list;     /* [N][G][pool_blocks] block numbers; entries from n_free on are not used */
+    int32_t *n_free;        /* [N][G]; the type of br_fscore's cap: workers without a free block are then not scored */
+} br_block_cache;
+
+/*
+ * Brings the block tables in line with the lengths: a request of n tokens holds need = ceil(n / block_tokens) blocks after it.
+ * Rows that hold more give back the blocks from column need on, rows that hold less grow.  Growth is served in slot order,
+ * from the blocks taken back in this call (in slot and column order), then from the end of the free list; those left over
+ * join the free list, the first of them last, so that undoing an update restores tables and lists.  A request whose growth
+ * no longer fits into what is left, in that order, or needs more than table_blocks columns, keeps what it holds and may be
+ * served by a later call; so do the growing requests behind one that does not fit.
+ *   n_blocks_out [N][G][B], n_free_out [N][G]   the counts after the update: cache->n_blocks and cache->n_free themselves, or
+ *                  other arrays.  With other arrays the old counts stay valid: the entries they reach are not written, so
+ *                  that an update can be looked at and dropped.
+ *   short_blocks   [N][G] blocks that requests of the worker still lack (2^31 - 1 if more); -1 if the worker's counts cannot
+ *                  be (outside their ranges, or more blocks held and free than the pool has), which leaves it as it was;
+ *                  may be NULL
+ * Entries of table and free_list that no count reaches are left as they were.
+ */
+int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const int32_t *len, const int32_t *step,
+                    int32_t *n_blocks_out, int32_t *n_free_out, int32_t *short_blocks);
+
+/*
+ * Where the newest tokens go: for each slot the last q tokens of its request, q = n_new [N][G][B] clipped to [0, n], or, with
+ * n_new NULL, the last token of each running request.  The tokens of a worker follow one another in slot and token order:
+ *   cu     [N][G][B + 1]  prefix sums of q (2^31 - 1 if more)
+ *   slots  [N][G][room]   table[b][p / block_tokens] * block_tokens + p % block_tokens of token p, -1 where the request holds
+ *                         no block for it.  Tokens from room on are dropped, entries behind the last token left as they were.
+ * The table is not written.  BR_EINVAL for room < 1.
+ */
+int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                const int32_t *n_new, int32_t room, int32_t *cu, int64_t *slots);
+
+/*
+ * The running requests of each worker packed in slot order, as an attention call over the paged cache reads them:
+ *   n_seq       [N][G]         running requests
+ *   seq_slot    [N][G][B]      the slot of each, -1 from n_seq on
+ *   indptr      [N][G][B + 1]  the blocks of request r are indices[indptr[r] .. indptr[r + 1]); rows from n_seq on are empty
+ *   indices     [N][G][pool_blocks]  block numbers; entries from indptr[B] on are left as they were
+ *   last_tokens [N][G][B]      tokens in the last of its blocks (0 without one, and from n_seq on)
+ * A request that holds fewer blocks than its tokens need is listed with what it holds, all of it full; one that holds more
+ * with what it needs.  The table is not written.
+ */
+int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                  int32_t *n_seq, int32_t *seq_slot, int32_t *indptr, int32_t *indices, int32_t *last_tokens);
+
+/*
  * Range-checked build (libbr_dbg.so, compiled with -DBR_BOUNDS; the paper has no counterpart).  In
  * that build every per-instance array of the step kernels -- shared memory and global rows -- is
  * indexed through a span that knows its length: an index outside it is counted and redirected to a

@@ -50,6 +50,11 @@ class BrInstanceBatch(C.Structure):
                 ("n_steps", C.c_int32), ("stream", C.c_void_p)]
 
 
+class BrBlockCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("G", "B", "block_tokens", "pool_blocks", "table_blocks")] + \
+               [(n, C.c_void_p) for n in ("table", "n_blocks", "free_list", "n_free")]
+
+
 class BrLoadOut(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("load", "trace", "status", "counters", "fscore",
                                           "phase_cycles")]
@@ -57,7 +62,8 @@ class BrLoadOut(C.Structure):
 
 EXPORTS = ["br_create", "br_step", "br_graph_capture", "br_graph_step", "br_step_host",
            "br_step_host_static", "br_debug_bounds_hits", "br_debug_bounds_selftest", "br_debug_step_registers",
-           "br_fscore", "br_best_subset", "br_bypass_dispatch", "br_survival_chat", "br_destroy", "br_strerror", "br_version"]
+           "br_fscore", "br_best_subset", "br_bypass_dispatch", "br_survival_chat", "br_block_tables",
+           "br_slot_map", "br_page_lists", "br_destroy", "br_strerror", "br_version"]
 
 _lib = None
 
@@ -92,6 +98,9 @@ def lib():
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.br_survival_chat.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
                                        C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.br_block_tables.argtypes = [C.c_void_p] * 7
+        L.br_slot_map.argtypes = [C.c_void_p] * 5 + [C.c_int32] + [C.c_void_p] * 2
+        L.br_page_lists.argtypes = [C.c_void_p] * 9
         L.br_debug_bounds_hits.argtypes = []
         L.br_debug_bounds_selftest.argtypes = [C.c_void_p]
         L.br_debug_step_registers.argtypes = [C.c_int32] * 5 + [C.POINTER(C.c_int32)]
@@ -120,6 +129,7 @@ _pack_batch = struct.Struct("@iiiP").pack
 _pack_state = struct.Struct("@11P").pack
 _pack_queue = struct.Struct("@4P").pack
 _pack_out = struct.Struct("@6P").pack
+_pack_cache = struct.Struct("@5i4x4P").pack
 
 
 def _addr(t) -> int:
@@ -340,6 +350,117 @@ class Router:
                                   _ptr(best_mask), _ptr(best_F))
         if rc != BR_OK:
             raise BrError(rc, "br_best_subset")
+
+
+class BlockCache:
+    """The paged caches of a batch of fleets (br_block_tables / br_slot_map / br_page_lists).
+
+    ``table`` [N, G, B, columns], ``n_blocks`` [N, G, B], ``free_list`` [N, G, pool] and ``n_free`` [N, G] are int32 tensors of
+    one device, contiguous, owned by the caller; ``block_tokens`` is the size of a cache block.  ``BlockCache.empty`` makes
+    the tensors of a new cache.  Every call takes the request lengths [N, G, B] as int32, plain or, with ``step`` [N], as the
+    router keeps them (``st["act_base"], step=st["step"]``), and works on the rows ``first`` to ``first + N``.  A tensor of
+    another type, shape, layout or device is refused with ValueError."""
+
+    def __init__(self, table, n_blocks, free_list, n_free, block_tokens):
+        import torch
+        self.torch, self._int32 = torch, torch.int32
+        if table.dim() != 4 or free_list.dim() != 3:
+            raise ValueError("BlockCache: table is [N, G, B, columns] and free_list [N, G, pool]")
+        self.device = table.device
+        self.N, self.G, self.B, self.columns = table.shape
+        self.pool, self.block_tokens = free_list.shape[2], int(block_tokens)
+        self._fleet, self._worker, self._slot = (self.N,), (self.N, self.G), (self.N, self.G, self.B)
+        self._cu = (self.N, self.G, self.B + 1)
+        self._check((table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
+                    (free_list, "free_list", (*self._worker, self.pool)), (n_free, "n_free", self._worker))
+        self.table, self.n_blocks, self.free_list, self.n_free = table, n_blocks, free_list, n_free
+        self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, table.data_ptr(),
+                                   n_blocks.data_ptr(), free_list.data_ptr(), n_free.data_ptr())
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+    @classmethod
+    def empty(cls, N, G, B, block_tokens, pool_blocks, table_blocks, device="cuda:0"):
+        """A new cache: no request holds a block, and the blocks are given out from number 0 up."""
+        import torch
+        z = dict(dtype=torch.int32, device=device)
+        free = torch.arange(pool_blocks - 1, -1, -1, **z).expand(N, G, pool_blocks).contiguous()
+        return cls(torch.zeros((N, G, B, table_blocks), **z), torch.zeros((N, G, B), **z), free,
+                   torch.full((N, G), pool_blocks, **z), block_tokens)
+
+    def _check(self, *arrays):
+        for t, name, shape in arrays:
+            if t.dtype is not self._int32 or t.shape != shape or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"{name}: needs a contiguous int32 tensor {list(shape)} on {self.device}, "
+                                 f"got {t.dtype} {list(t.shape)} on {t.device}")
+
+    def _batch(self, N, first, stream):
+        if N is None:
+            N = self.N - first
+        if first < 0 or N < 0 or first + N > self.N:
+            raise ValueError(f"rows {first} to {first + N}: the cache has {self.N}")
+        if stream is None:
+            if self.device.type != "cuda":
+                stream = 0
+            elif self._raw_stream is not None:
+                stream = self._raw_stream(self.device.index)
+            else:
+                stream = self.torch.cuda.current_stream(self.device).cuda_stream
+        elif isinstance(stream, C.c_void_p):
+            stream = stream.value or 0
+        elif hasattr(stream, "cuda_stream"):
+            stream = stream.cuda_stream
+        return _pack_batch(N, first, 1, stream)
+
+    def _call(self, name, *args):
+        if self.N == 0:
+            return                                           # (empty tensors have no address)
+        fn = getattr(lib(), name)
+        if self.device.type == "cuda" and self.torch.cuda.current_device() != self.device.index:
+            with self.torch.cuda.device(self.device):       # the launch goes to the tensors' device
+                rc = fn(*args)
+        else:
+            rc = fn(*args)
+        if rc != BR_OK:
+            raise BrError(rc, name)
+
+    def block_tables(self, length, n_blocks_out=None, n_free_out=None, short_blocks=None, step=None, N=None, first=0,
+                     stream=None):
+        """Brings tables and free lists in line with the lengths; the new counts go to ``n_blocks_out`` and ``n_free_out``
+        (default: the cache's own, in place)."""
+        nb = self.n_blocks if n_blocks_out is None else n_blocks_out
+        nf = self.n_free if n_free_out is None else n_free_out
+        self._check((length, "length", self._slot), (nb, "n_blocks_out", self._slot), (nf, "n_free_out", self._worker))
+        if step is not None:
+            self._check((step, "step", self._fleet))
+        if short_blocks is not None:
+            self._check((short_blocks, "short_blocks", self._worker))
+        self._call("br_block_tables", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step),
+                   nb.data_ptr(), nf.data_ptr(), _ptr(short_blocks))
+
+    def slot_map(self, length, cu, slots, n_new=None, step=None, N=None, first=0, stream=None):
+        """Cache slots of the newest ``n_new`` tokens of each request (default: one of each running request) into ``slots``
+        [N, G, room] int64, with prefix sums ``cu`` [N, G, B + 1]."""
+        self._check((length, "length", self._slot), (cu, "cu", self._cu))
+        if n_new is not None:
+            self._check((n_new, "n_new", self._slot))
+        if step is not None:
+            self._check((step, "step", self._fleet))
+        if slots.dtype is not self.torch.int64 or slots.dim() != 3 or slots.shape[:2] != self._worker or \
+                slots.device != self.device or not slots.is_contiguous():
+            raise ValueError(f"slots: needs a contiguous int64 tensor [{self.N}, {self.G}, room] on {self.device}, "
+                             f"got {slots.dtype} {list(slots.shape)} on {slots.device}")
+        self._call("br_slot_map", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step), _ptr(n_new),
+                   slots.shape[2], cu.data_ptr(), slots.data_ptr())
+
+    def page_lists(self, length, n_seq, seq_slot, indptr, indices, last_tokens, step=None, N=None, first=0, stream=None):
+        """The running requests packed, with their blocks one after another."""
+        self._check((length, "length", self._slot), (n_seq, "n_seq", self._worker), (seq_slot, "seq_slot", self._slot),
+                    (indptr, "indptr", self._cu), (indices, "indices", (self.N, self.G, self.pool)),
+                    (last_tokens, "last_tokens", self._slot))
+        if step is not None:
+            self._check((step, "step", self._fleet))
+        self._call("br_page_lists", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step),
+                   n_seq.data_ptr(), seq_slot.data_ptr(), indptr.data_ptr(), indices.data_ptr(), last_tokens.data_ptr())
 
 
 def state_to_numpy(st) -> Dict[str, np.ndarray]:

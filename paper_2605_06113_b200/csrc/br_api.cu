@@ -16,6 +16,7 @@
 #include "br_subset.cuh"
 #include "br_bypass.cuh"
 #include "br_survival.cuh"
+#include "br_cache.cuh"
 
 using br::StepArgs;
 
@@ -822,6 +823,81 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
     br::br_survival_kernel<<<(unsigned)blocks, 256, 0, (cudaStream_t)stream>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "br_survival_chat launch");
+    return BR_OK;
+}
+
+// What the three calls on block caches have in common: checks, and the part of the arguments that they share.
+static int cache_args(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                      br::CacheArgs *c)
+{
+    if (!batch || !cache || !len || !cache->table || !cache->n_blocks || !cache->free_list || !cache->n_free) return BR_EINVAL;
+    if (batch->n_instances < 0 || batch->first_instance < 0) return BR_EINVAL;
+    if (cache->G < 1 || cache->G > BR_MAX_G || cache->B < 1 || cache->B > BR_MAX_B) return BR_EINVAL;
+    if (cache->block_tokens < 1 || cache->block_tokens > BR_MAX_BLOCK_TOKENS || cache->table_blocks < 1 ||
+        cache->table_blocks > BR_MAX_TABLE_BLOCKS || cache->pool_blocks < 1 || cache->pool_blocks > BR_MAX_POOL_BLOCKS)
+        return BR_EINVAL;
+    if (misaligned(len, 4) || misaligned(step, 4) || misaligned(cache->table, 4) || misaligned(cache->n_blocks, 4) ||
+        misaligned(cache->free_list, 4) || misaligned(cache->n_free, 4))
+        return BR_EINVAL;
+    // (rows are counted in 32 bits; the offsets into the arrays are not)
+    if (((int64_t)batch->first_instance + batch->n_instances) * cache->G > 0x7FFFFFFF) return BR_EINVAL;
+    c->G = cache->G; c->B = cache->B; c->t = cache->block_tokens; c->T = cache->table_blocks; c->P = cache->pool_blocks;
+    c->first_row = batch->first_instance * cache->G;
+    c->len = len; c->step = step;
+    c->table = cache->table; c->n_blocks = cache->n_blocks; c->free_list = cache->free_list; c->n_free = cache->n_free;
+    return BR_OK;
+}
+
+int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const int32_t *len, const int32_t *step,
+                    int32_t *n_blocks_out, int32_t *n_free_out, int32_t *short_blocks)
+{
+    br::TableArgs a;
+    const int rc = cache_args(batch, cache, len, step, &a.c);
+    if (rc != BR_OK) return rc;
+    if (!n_blocks_out || !n_free_out) return BR_EINVAL;
+    if (misaligned(n_blocks_out, 4) || misaligned(n_free_out, 4) || misaligned(short_blocks, 4)) return BR_EINVAL;
+    const int64_t workers = (int64_t)batch->n_instances * cache->G;
+    if (workers == 0) return BR_OK;
+    a.n_blocks_out = n_blocks_out; a.n_free_out = n_free_out; a.short_out = short_blocks;
+    br::br_block_tables_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "br_block_tables launch");
+    return BR_OK;
+}
+
+int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                const int32_t *n_new, int32_t room, int32_t *cu, int64_t *slots)
+{
+    br::SlotArgs a;
+    const int rc = cache_args(batch, cache, len, step, &a.c);
+    if (rc != BR_OK) return rc;
+    if (!cu || !slots || room < 1) return BR_EINVAL;
+    if (misaligned(n_new, 4) || misaligned(cu, 4) || misaligned(slots, 8)) return BR_EINVAL;
+    const int64_t workers = (int64_t)batch->n_instances * cache->G;
+    if (workers == 0) return BR_OK;
+    a.n_new = n_new; a.room = room; a.cu = cu; a.slots = slots;
+    br::br_slot_map_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "br_slot_map launch");
+    return BR_OK;
+}
+
+int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                  int32_t *n_seq, int32_t *seq_slot, int32_t *indptr, int32_t *indices, int32_t *last_tokens)
+{
+    br::PageArgs a;
+    const int rc = cache_args(batch, cache, len, step, &a.c);
+    if (rc != BR_OK) return rc;
+    if (!n_seq || !seq_slot || !indptr || !indices || !last_tokens) return BR_EINVAL;
+    if (misaligned(n_seq, 4) || misaligned(seq_slot, 4) || misaligned(indptr, 4) || misaligned(indices, 4) ||
+        misaligned(last_tokens, 4))
+        return BR_EINVAL;
+    const int64_t workers = (int64_t)batch->n_instances * cache->G;
+    if (workers == 0) return BR_OK;
+    a.n_seq = n_seq; a.seq_slot = seq_slot; a.indptr = indptr; a.indices = indices; a.last = last_tokens;
+    br::br_page_lists_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "br_page_lists launch");
     return BR_OK;
 }
 

@@ -1,0 +1,359 @@
+"""Block tables, slot maps and page lists against their definitions, worked out request by request in Python integers.  All
+outputs are whole numbers, so the tolerance is equality, untouched entries included."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_06113_b200 import workload as wlm
+from paper_2605_06113_b200.binding import BlockCache, Router
+
+import cache_reference as ref
+from cache_reference import EMPTY, MOST
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+# N, G, B, tokens a block, blocks a pool, columns a row
+SHAPES = [(1, 1, 1, 1, 1, 1), (1, 4, 64, 16, 700, 90), (3, 5, 7, 24, 60, 31), (2, 3, 256, 16, 5000, 65), (70, 33, 8, 5, 97, 40),
+          (300, 9, 33, 64, 150, 17), (1, 64, 40, 1, 900, 333), (2, 1, 65, 128, 4099, 1030), (1, 2, 9, 100, 3000, 2500),
+          (2500, 8, 16, 16, 64, 9), (5, 1, 255, 7, 33, 6), (1, 1, 130, 3, 20011, 1000)]
+
+
+def _gpu(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+class Pair:
+    """A cache on the GPU and its host copy."""
+
+    def __init__(self, N, G, B, t, P, T, seed=0):
+        self.f = ref.Fleets(N, G, B, t, P, T)
+        rng = np.random.default_rng(seed)
+        for at in self.f.workers():
+            rng.shuffle(self.f.free_list[at])
+        self.c = BlockCache(_gpu(self.f.table), _gpu(self.f.n_blocks), _gpu(self.f.free_list), _gpu(self.f.n_free), t)
+
+    def same(self, nb=None, nf=None):
+        f, c = self.f, self.c
+        for name, have, want in (("table", c.table, f.table), ("free_list", c.free_list, f.free_list),
+                                 ("n_blocks", c.n_blocks if nb is None else nb[0], f.n_blocks if nb is None else nb[1]),
+                                 ("n_free", c.n_free if nf is None else nf[0], f.n_free if nf is None else nf[1])):
+            assert np.array_equal(have.cpu().numpy(), want), name
+
+    def update(self, length, step=None, out=False, **kw):
+        c, f = self.c, self.f
+        short = torch.full((f.N, f.G), -77, dtype=torch.int32, device=DEV)
+        nb, nf = (c.n_blocks.clone(), c.n_free.clone()) if out else (None, None)
+        c.block_tables(_gpu(length), nb, nf, short, step=None if step is None else _gpu(step), **kw)
+        wnb, wnf, wshort = f.update(length, step, commit=not out, **{k: v for k, v in kw.items() if k != "stream"})
+        assert np.array_equal(short.cpu().numpy(), wshort)
+        self.same((nb, wnb) if out else None, (nf, wnf) if out else None)
+        if out:
+            self.same()
+        return wshort
+
+    def slots(self, length, room, n_new=None, step=None, **kw):
+        c, f = self.c, self.f
+        cu = torch.full((f.N, f.G, f.B + 1), -7, dtype=torch.int32, device=DEV)
+        out = torch.full((f.N, f.G, room), -7, dtype=torch.int64, device=DEV)
+        c.slot_map(_gpu(length), cu, out, n_new=None if n_new is None else _gpu(n_new), step=None if step is None else _gpu(step), **kw)
+        wcu, wout = f.slots(length, room, n_new, step, **kw)
+        assert np.array_equal(cu.cpu().numpy(), wcu)
+        assert np.array_equal(out.cpu().numpy(), wout)
+
+    def pages(self, length, step=None, **kw):
+        c, f = self.c, self.f
+        z = dict(dtype=torch.int32, device=DEV)
+        o = [torch.full(s, -7, **z) for s in ((f.N, f.G), (f.N, f.G, f.B), (f.N, f.G, f.B + 1), (f.N, f.G, f.P), (f.N, f.G, f.B))]
+        c.page_lists(_gpu(length), *o, step=None if step is None else _gpu(step), **kw)
+        for name, have, want in zip(("n_seq", "seq_slot", "indptr", "indices", "last_tokens"), o, f.pages(length, step, **kw)):
+            assert np.array_equal(have.cpu().numpy(), want), name
+
+
+def _walk(rng, f, n, ended, refill, grow):
+    """The next lengths: requests end, slots are refilled, the others grow; sizes that use the pool up now and then."""
+    most = min(f.T * f.t, int(2.2 * f.P * f.t / f.B) + 2)
+    n = np.where((n > 0) & (rng.random(n.shape) >= ended), n + grow, 0)
+    return np.where((n == 0) & (rng.random(n.shape) < refill), rng.integers(0, most + 1, n.shape), n)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("stepped", [False, True])
+def test_walks_of_lengths(shape, stepped):
+    p = Pair(*shape, seed=sum(shape))
+    f = p.f
+    rng = np.random.default_rng(17 * sum(shape) + stepped)
+    n = np.zeros((f.N, f.G, f.B), np.int64)
+    big = f.N * f.G > 500
+    for k, (ended, refill, grow) in enumerate([(0, 0.7, 1), (0.0, 0.0, 1), (0.3, 0.6, 5), (0.01, 0.1, 1), (0.9, 0.2, 40)][:3 if big else 5]):
+        n = _walk(rng, f, n, ended, refill, grow)
+        step = rng.integers(-5, 10 ** 6, f.N).astype(np.int32) if stepped else None
+        length = (np.where(n > 0, n - step[:, None, None], EMPTY) if stepped else n).astype(np.int32)
+        if k % 2:
+            p.update(length, step, out=True)                     # looked at and dropped
+        p.update(length, step)
+        n_new = rng.integers(-2, 60, n.shape).astype(np.int32)
+        if k == 2:
+            n_new = np.where(rng.random(n.shape) < 0.5, MOST, 0).astype(np.int32)
+        p.slots(length, f.B, step=step)
+        p.slots(length, int(rng.integers(1, 30 * f.B + 2)), n_new, step)
+        p.pages(length, step)
+        if not big:
+            f.check_partition()
+    later = (length + (length != EMPTY) * 3).astype(np.int32)    # tables that are behind the lengths, and ahead of them
+    p.slots(later, 2 * f.B + 1, n_new, step)
+    p.pages(later, step)
+    earlier = (np.where(length == EMPTY, EMPTY, length // 2) if not stepped else length - 2 * (length != EMPTY)).astype(np.int32)
+    p.slots(earlier, 2 * f.B + 1, n_new, step)
+    p.pages(earlier, step)
+
+
+@pytest.mark.parametrize("N,G", [(1, 1), (2, 64), (40, 64), (700, 8)])
+def test_one_request_takes_the_whole_pool_and_gives_it_back(N, G):
+    p = Pair(N, G, 24, 16, 1500, 1500, seed=N)
+    n = np.zeros((N, G, 24), np.int32)
+    n[:, :, 5] = 1500 * 16
+    p.update(n)
+    p.pages(n)
+    p.slots(n, 300, np.full(n.shape, 301, np.int32))
+    m = n.copy()
+    m[:, :, 5] = 0
+    m[:, :, 23] = 1499 * 16 + 1
+    p.update(m, out=True)
+    p.update(m)                                                  # all of its blocks go to another slot
+    m[:, :, 3] = 1
+    assert (p.update(m) == 1).all()                              # nothing left for one more
+    p.update(np.zeros_like(m))
+    p.f.check_partition()
+
+
+def test_undoing_an_update_restores_tables_and_lists():
+    p = Pair(6, 20, 64, 16, 900, 60, seed=3)
+    rng = np.random.default_rng(4)
+    A = rng.integers(0, 200, (6, 20, 64)).astype(np.int32)
+    p.update(A)
+    table, free = p.c.table.clone(), p.c.free_list.clone()
+    nb, nf = p.c.n_blocks.clone(), p.c.n_free.clone()
+    p.update((A + rng.integers(-90, 40, A.shape)).astype(np.int32))
+    p.update(A)
+    assert torch.equal(nb, p.c.n_blocks) and torch.equal(nf, p.c.n_free)
+    held = torch.arange(60, device=DEV) < nb[..., None]
+    listed = torch.arange(900, device=DEV) < nf[..., None]
+    assert torch.equal(torch.where(held, table, 0), torch.where(held, p.c.table, 0))
+    assert torch.equal(torch.where(listed, free, 0), torch.where(listed, p.c.free_list, 0))
+
+
+@pytest.mark.parametrize("workers", [(1, 3), (900, 7)])
+def test_counts_that_cannot_be_leave_the_worker_as_it_was(workers):
+    N, G = workers
+    for k, (name, value) in enumerate([("n_free", -1), ("n_free", 51), ("n_blocks", -1), ("n_blocks", 11), ("n_blocks", MOST),
+                                       ("n_free", MOST), ("n_free", 45), ("n_blocks", -(2 ** 31))]):
+        p = Pair(N, G, 12, 4, 50, 10, seed=k)
+        n = np.full((N, G, 12), 3, np.int32)
+        p.update(n)
+        getattr(p.f, name)[N - 1, G - 1, ...] = value
+        getattr(p.c, name)[N - 1, G - 1, ...] = value
+        n[:, :, 2] = 0
+        n[:, :, 7] = 21
+        for out in (True, False):
+            short = p.update(n, out=out)
+            assert short[N - 1, G - 1] == -1 and (short.ravel()[:-1] == 0).all()
+        p.slots(n, 40, np.full(n.shape, 3, np.int32))            # counts are clipped to the row
+        p.pages(n)
+
+
+def test_lengths_at_the_ends_of_their_range():
+    N, G, B = 5, 2, 10
+    edge = np.array([EMPTY, EMPTY + 1, -1, 0, 1, MOST, MOST - 5, 15, 16, 17], np.int32)
+    length = np.tile(edge, (N, G, 1))
+    step = np.array([0, 1, MOST, -(2 ** 31), -16], np.int32)
+    for t in (16, 1, 1 << 20, (1 << 20) - 1):
+        p = Pair(N, G, B, t, 4100, 2048, seed=t)
+        p.update(length, step)
+        p.update(length)
+        p.slots(length, 50, np.full((N, G, B), 5, np.int32), step)
+        p.slots(length, 10)
+        p.pages(length, step)
+    # sums of new tokens beyond 2^31 - 1
+    p.slots(np.full((N, G, B), MOST, np.int32), 7, np.array([3] + [MOST] * 9, np.int32) * np.ones((N, G, 1), np.int32))
+
+
+def test_cache_slots_beyond_32_bits():
+    t = 1 << 20
+    p = Pair(2, 3, 4, t, 5000, 2048, seed=9)                      # block 4999 starts at slot 5.2e9
+    n = np.array([MOST, 5, t, t + 1], np.int32) * np.ones((2, 3, 1), np.int32)
+    p.update(n)
+    p.slots(n, 4000, np.full(n.shape, 999, np.int32))
+    assert (p.f.table[p.f.table >= 0].astype(np.int64) * t).max() > 2 ** 32
+
+
+def test_tables_beyond_32_bits():
+    G, B, T = 64, 256, 140001                                     # 2.29e9 entries
+    z = dict(dtype=torch.int32, device=DEV)
+    c = BlockCache(torch.empty((1, G, B, T), **z), torch.zeros((1, G, B), **z),
+                   torch.arange(999, -1, -1, **z).expand(1, G, 1000).contiguous(), torch.full((1, G), 1000, **z), 16)
+    length = torch.zeros((1, G, B), **z)
+    length[:, :, 254] = 16 * 900 + 3
+    length[:, :, 255] = 16 * 20
+    c.block_tables(length)
+    assert c.n_blocks[0, :, 254].tolist() == [901] * G and c.n_blocks[0, :, 255].tolist() == [20] * G
+    assert torch.equal(c.table[0, :, 254, :901], torch.arange(901, **z).expand(G, 901))
+    assert torch.equal(c.table[0, :, 255, :20], torch.arange(901, 921, **z).expand(G, 20))
+    cu, slots = torch.zeros((1, G, B + 1), **z), torch.zeros((1, G, 64), dtype=torch.int64, device=DEV)
+    c.slot_map(length, cu, slots)
+    assert slots[0, :, :2].tolist() == [[900 * 16 + 2, 921 * 16 - 1]] * G
+    o = [torch.zeros(s, **z) for s in ((1, G), (1, G, B), (1, G, B + 1), (1, G, 1000), (1, G, B))]
+    c.page_lists(length, *o)
+    assert torch.equal(o[3][0, :, :921], torch.arange(921, **z).expand(G, 921)) and o[0].tolist() == [[2] * G]
+    c.block_tables(torch.zeros_like(length))
+    assert c.n_free.tolist() == [[1000] * G] and torch.equal(c.free_list[0, 0], torch.arange(999, -1, -1, **z))
+
+
+@pytest.mark.parametrize("shape", [(7, 3, 20, 8, 80, 30), (500, 10, 8, 8, 40, 12)])
+def test_rows_of_a_batch(shape):
+    p = Pair(*shape, seed=11)
+    f = p.f
+    rng = np.random.default_rng(1)
+    n = rng.integers(0, 60, (f.N, f.G, f.B)).astype(np.int32)
+    step = rng.integers(0, 9, f.N).astype(np.int32)
+    q = rng.integers(0, 9, n.shape).astype(np.int32)
+    for first, N in ((2, 3), (0, 1), (f.N - 1, 1), (4, None)):
+        rows = dict(first=first, N=f.N - first if N is None else N)
+        p.update(n, step, **rows)
+        p.slots(n, 37, q, step, **rows)
+        p.pages(n, step, **rows)
+    p.update(n, step, first=3, N=0)
+
+
+def test_unaligned_tensors():
+    """Arrays that start at any multiple of their elements' size, as slices of a larger buffer do."""
+    shape = N, G, B, t, P, T = 3, 5, 23, 16, 301, 40
+    rng = np.random.default_rng(2)
+    for off in (1, 2, 3):
+        p = Pair(*shape, seed=off)
+
+        def shifted(a):
+            flat = torch.zeros(a.numel() + 4, dtype=a.dtype, device=DEV)
+            v = flat[off:off + a.numel()].view(a.shape)
+            v.copy_(a)
+            return v
+
+        p.c = BlockCache(shifted(p.c.table), shifted(p.c.n_blocks), shifted(p.c.free_list), shifted(p.c.n_free), t)
+        n = rng.integers(0, 300, (N, G, B)).astype(np.int32)
+        nb, nf = shifted(p.c.n_blocks), shifted(p.c.n_free)
+        p.c.block_tables(shifted(_gpu(n)), nb, nf)
+        wnb, wnf, _ = p.f.update(n, commit=False)
+        p.same((nb, wnb), (nf, wnf))
+        p.update(n)
+        cu, out = (shifted(torch.full(s, -7, dtype=d, device=DEV)) for s, d in (((N, G, B + 1), torch.int32), ((N, G, 1001), torch.int64)))
+        p.c.slot_map(shifted(_gpu(n)), cu, out, n_new=shifted(_gpu(n)))
+        for have, want in zip((cu, out), p.f.slots(n, 1001, n)):
+            assert np.array_equal(have.cpu().numpy(), want)
+        o = [shifted(torch.full(s, -7, dtype=torch.int32, device=DEV)) for s in ((N, G), (N, G, B), (N, G, B + 1), (N, G, P), (N, G, B))]
+        p.c.page_lists(shifted(_gpu(n)), *o)
+        for have, want in zip(o, p.f.pages(n)):
+            assert np.array_equal(have.cpu().numpy(), want)
+
+
+def test_lengths_written_by_the_kernel_ahead_and_other_streams():
+    shape = N, G, B, t, P, T = 40, 16, 64, 16, 600, 20
+    p = Pair(*shape, seed=21)
+    rng = np.random.default_rng(3)
+    base = rng.integers(0, 130, (N, G, B)).astype(np.int32)
+    lens, src = torch.empty((N, G, B), dtype=torch.int32, device=DEV), _gpu(base)
+    side = torch.cuda.Stream()
+    out = torch.zeros((12, N, G, B), dtype=torch.int64, device=DEV)
+    cu = torch.zeros((N, G, B + 1), dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for k in range(12):                                       # nothing waits for the host in between
+            torch.add(src, k, out=lens)
+            p.c.block_tables(lens)
+            p.c.slot_map(lens, cu, out[k])
+    side.synchronize()
+    for k in range(12):
+        p.f.update((base + k).astype(np.int32))
+        assert np.array_equal(out[k].cpu().numpy(), p.f.slots((base + k).astype(np.int32), B, fill=0)[1]), k
+    p.same()
+    explicit = torch.cuda.Stream()
+    p.update(base, stream=explicit)
+    explicit.synchronize()
+
+
+def test_captured_and_replayed():
+    shape = N, G, B, t, P, T = 20, 16, 64, 16, 500, 30
+    p = Pair(*shape, seed=31)
+    rng = np.random.default_rng(6)
+    base = rng.integers(0, 100, (N, G, B)).astype(np.int32)
+    lens, step = _gpu(base), torch.zeros(N, dtype=torch.int32, device=DEV)
+    z = dict(dtype=torch.int32, device=DEV)
+    cu, out, short = torch.zeros((N, G, B + 1), **z), torch.zeros((N, G, B), dtype=torch.int64, device=DEV), torch.zeros((N, G), **z)
+    o = [torch.full(s, -7, **z) for s in ((N, G), (N, G, B), (N, G, B + 1), (N, G, P), (N, G, B))]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step.add_(1)
+        p.c.block_tables(lens, short_blocks=short, step=step)
+        p.c.slot_map(lens, cu, out, step=step)
+        p.c.page_lists(lens, *o, step=step)
+    for k in range(1, 30):
+        if k == 9:
+            base = rng.integers(0, 100, (N, G, B)).astype(np.int32)
+            lens.copy_(_gpu(base))
+        graph.replay()
+        host_step = np.full(N, k, np.int32)
+        p.f.update(base, host_step)
+        if k in (1, 9, 29):
+            torch.cuda.synchronize()
+            p.same()
+            wcu, wout = p.f.slots(base, B, step=host_step, fill=0)
+            running = np.arange(B) < wcu[..., -1:]
+            assert np.array_equal(cu.cpu().numpy(), wcu) and np.array_equal(np.where(running, out.cpu().numpy(), 0), wout)
+            want = p.f.pages(base, host_step)
+            for have, w in zip((o[0], o[1], o[2], o[4]), (want[0], want[1], want[2], want[4])):
+                assert np.array_equal(have.cpu().numpy(), w)
+            used = np.arange(P) < want[2][..., -1:]
+            assert np.array_equal(np.where(used, o[3].cpu().numpy(), -7), want[3])
+
+
+@pytest.mark.parametrize("name,kw,n_inst,steps", [("c0", dict(hazard=0.05), 1, 40), ("c3", dict(hazard=0.1, G=5, init_active=40), 3, 25)])
+def test_beside_the_routing_step(name, kw, n_inst, steps):
+    """Route, bring the tables up to date, map the new tokens, list the pages, step after step on the router's own state; the
+    free blocks then say which workers an F-score call may choose."""
+    cfg = wlm.get_config(name, **kw)
+    wl = wlm.make_workload(cfg, n_instances=n_inst)
+    r = Router(wl, device=DEV)
+    st, out = r.device_state(), r.outputs(n_inst)
+    p = Pair(n_inst, cfg.G, cfg.B, 16, 2600, 2100, seed=41)
+    z = dict(dtype=torch.int32, device=DEV)
+    f = p.f
+    cu, slots = torch.zeros((n_inst, f.G, f.B + 1), **z), torch.zeros((n_inst, f.G, f.B), dtype=torch.int64, device=DEV)
+    o = [torch.zeros(s, **z) for s in ((n_inst, f.G), (n_inst, f.G, f.B), (n_inst, f.G, f.B + 1), (n_inst, f.G, f.P), (n_inst, f.G, f.B))]
+    for k in range(steps):
+        r.step(st, out)
+        p.c.block_tables(st["act_base"], step=st["step"])
+        p.c.slot_map(st["act_base"], cu, slots, step=st["step"])
+        p.c.page_lists(st["act_base"], *o, step=st["step"])
+        base, step = st["act_base"].cpu().numpy(), st["step"].cpu().numpy()
+        assert (step == k + 1).all()
+        f.update(base, step)
+        p.same()
+        wcu, wout = f.slots(base, f.B, step=step, fill=0)
+        live = np.arange(f.B) < wcu[..., -1:]
+        assert np.array_equal(cu.cpu().numpy(), wcu) and np.array_equal(np.where(live, slots.cpu().numpy(), 0), wout)
+        want = f.pages(base, step, fill=0)
+        assert np.array_equal(o[0].cpu().numpy(), st["nact"].cpu().numpy())
+        for j in (0, 1, 2, 4):
+            assert np.array_equal(o[j].cpu().numpy(), want[j])
+        used = np.arange(f.P) < want[2][..., -1:]
+        assert np.array_equal(np.where(used, o[3].cpu().numpy(), 0), want[3])
+    f.check_partition()
+    p.c.n_free[:, 1] = 0                                          # a worker whose pool is used up takes no request
+    s = torch.full((n_inst, 8), 100, **z)
+    best = torch.zeros((n_inst, 8), **z)
+    F = torch.zeros((n_inst, 8, f.G), dtype=torch.float64, device=DEV)
+    load = torch.arange(f.G, dtype=torch.int64, device=DEV).flip(0).mul(1000).expand(n_inst, f.G).contiguous()
+    load[:, 1] = -10 ** 6
+    r.fscore(s, load, F, cap=p.c.n_free, best_g=best)
+    assert not bool((best == 1).any())
+    r.close()
