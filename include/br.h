@@ -316,6 +316,7 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
 #define BR_MAX_BLOCK_TOKENS (1 << 20)
 #define BR_MAX_TABLE_BLOCKS (1 << 22)
 #define BR_MAX_POOL_BLOCKS  (1 << 28)
+#define BR_MAX_SLOT_ROOM    (1 << 30)
 
 typedef struct {
     int32_t  G, B;          /* workers per instance and slots per worker: 1 <= G <= BR_MAX_G, 1 <= B <= BR_MAX_B */
@@ -352,7 +353,7 @@ int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const
  *   cu     [N][G][B + 1]  prefix sums of q (2^31 - 1 if more)
  *   slots  [N][G][room]   table[b][p / block_tokens] * block_tokens + p % block_tokens of token p, -1 where the request holds
  *                         no block for it.  Tokens from room on are dropped, entries behind the last token left as they were.
- * The table is not written.  BR_EINVAL for room < 1.
+ * The table is not written.  BR_EINVAL for room outside [1, BR_MAX_SLOT_ROOM].
  */
 int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
                 const int32_t *n_new, int32_t room, int32_t *cu, int64_t *slots);

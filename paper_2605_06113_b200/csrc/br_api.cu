@@ -222,6 +222,46 @@ int launch_step(br_ctx *ctx, const br_instance_batch *b, const br_worker_state *
     return BR_OK;
 }
 
+// What the three calls on block caches have in common: checks, and the part of the arguments that they share.
+int cache_args(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
+                      br::CacheArgs *c)
+{
+    if (!batch || !cache || !len || !cache->table || !cache->n_blocks || !cache->free_list || !cache->n_free) return BR_EINVAL;
+    if (batch->n_instances < 0 || batch->first_instance < 0) return BR_EINVAL;
+    if (cache->G < 1 || cache->G > BR_MAX_G || cache->B < 1 || cache->B > BR_MAX_B) return BR_EINVAL;
+    if (cache->block_tokens < 1 || cache->block_tokens > BR_MAX_BLOCK_TOKENS || cache->table_blocks < 1 ||
+        cache->table_blocks > BR_MAX_TABLE_BLOCKS || cache->pool_blocks < 1 || cache->pool_blocks > BR_MAX_POOL_BLOCKS)
+        return BR_EINVAL;
+    if (misaligned(len, 4) || misaligned(step, 4) || misaligned(cache->table, 4) || misaligned(cache->n_blocks, 4) ||
+        misaligned(cache->free_list, 4) || misaligned(cache->n_free, 4))
+        return BR_EINVAL;
+    // (rows are counted in 32 bits; the offsets into the arrays are not)
+    if (((int64_t)batch->first_instance + batch->n_instances) * cache->G > 0x7FFFFFFF) return BR_EINVAL;
+    c->G = cache->G; c->B = cache->B; c->t = cache->block_tokens; c->T = cache->table_blocks; c->P = cache->pool_blocks;
+    c->first_row = batch->first_instance * cache->G; c->workers = batch->n_instances * cache->G; c->parts = 1;
+    br::cache_divisor(cache->block_tokens, &c->t_magic, &c->t_shift);
+    c->len = len; c->step = step;
+    c->table = cache->table; c->n_blocks = cache->n_blocks; c->free_list = cache->free_list; c->n_free = cache->n_free;
+    return BR_OK;
+}
+
+// Slots per lane of the cache kernels: the smallest power of two that takes B slots with a warp.
+#define BR_BY_SLOTS(kernel, B) ((B) <= 32 ? br::kernel<1> : (B) <= 64 ? br::kernel<2> : (B) <= 128 ? br::kernel<4> : br::kernel<8>)
+
+template <typename Args>
+int launch_cache(void (*kern)(const Args), const Args &a, int warps, size_t smem, const br_instance_batch *batch,
+                        const char *what)
+{
+    const int64_t blocks = ((int64_t)a.c.workers * a.c.parts + warps - 1) / warps;
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    BR_CUDA(cudaStreamIsCapturing((cudaStream_t)batch->stream, &capturing));
+    cudaError_t e = launch_overlapped(kern, dim3((unsigned)blocks), 32 * warps, smem, (cudaStream_t)batch->stream, a,
+                                      capturing == cudaStreamCaptureStatusNone);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, what);
+    return BR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -826,28 +866,6 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
     return BR_OK;
 }
 
-// What the three calls on block caches have in common: checks, and the part of the arguments that they share.
-static int cache_args(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
-                      br::CacheArgs *c)
-{
-    if (!batch || !cache || !len || !cache->table || !cache->n_blocks || !cache->free_list || !cache->n_free) return BR_EINVAL;
-    if (batch->n_instances < 0 || batch->first_instance < 0) return BR_EINVAL;
-    if (cache->G < 1 || cache->G > BR_MAX_G || cache->B < 1 || cache->B > BR_MAX_B) return BR_EINVAL;
-    if (cache->block_tokens < 1 || cache->block_tokens > BR_MAX_BLOCK_TOKENS || cache->table_blocks < 1 ||
-        cache->table_blocks > BR_MAX_TABLE_BLOCKS || cache->pool_blocks < 1 || cache->pool_blocks > BR_MAX_POOL_BLOCKS)
-        return BR_EINVAL;
-    if (misaligned(len, 4) || misaligned(step, 4) || misaligned(cache->table, 4) || misaligned(cache->n_blocks, 4) ||
-        misaligned(cache->free_list, 4) || misaligned(cache->n_free, 4))
-        return BR_EINVAL;
-    // (rows are counted in 32 bits; the offsets into the arrays are not)
-    if (((int64_t)batch->first_instance + batch->n_instances) * cache->G > 0x7FFFFFFF) return BR_EINVAL;
-    c->G = cache->G; c->B = cache->B; c->t = cache->block_tokens; c->T = cache->table_blocks; c->P = cache->pool_blocks;
-    c->first_row = batch->first_instance * cache->G;
-    c->len = len; c->step = step;
-    c->table = cache->table; c->n_blocks = cache->n_blocks; c->free_list = cache->free_list; c->n_free = cache->n_free;
-    return BR_OK;
-}
-
 int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const int32_t *len, const int32_t *step,
                     int32_t *n_blocks_out, int32_t *n_free_out, int32_t *short_blocks)
 {
@@ -856,13 +874,12 @@ int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const
     if (rc != BR_OK) return rc;
     if (!n_blocks_out || !n_free_out) return BR_EINVAL;
     if (misaligned(n_blocks_out, 4) || misaligned(n_free_out, 4) || misaligned(short_blocks, 4)) return BR_EINVAL;
-    const int64_t workers = (int64_t)batch->n_instances * cache->G;
-    if (workers == 0) return BR_OK;
+    if (a.c.workers == 0) return BR_OK;
     a.n_blocks_out = n_blocks_out; a.n_free_out = n_free_out; a.short_out = short_blocks;
-    br::br_block_tables_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, "br_block_tables launch");
-    return BR_OK;
+    a.c.parts = br::cache_table_parts(a.c.workers);
+    const int warps = a.c.parts > 1 ? a.c.parts : br::kCacheThreads / 32;
+    const size_t smem = (size_t)(a.c.parts > 1 ? 1 : warps) * 2 * cache->B * sizeof(br::Run);     // at most 32 KB
+    return launch_cache(BR_BY_SLOTS(br_block_tables_kernel, cache->B), a, warps, smem, batch, "br_block_tables launch");
 }
 
 int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
@@ -871,15 +888,16 @@ int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, con
     br::SlotArgs a;
     const int rc = cache_args(batch, cache, len, step, &a.c);
     if (rc != BR_OK) return rc;
-    if (!cu || !slots || room < 1) return BR_EINVAL;
+    if (!cu || !slots || room < 1 || room > BR_MAX_SLOT_ROOM) return BR_EINVAL;
     if (misaligned(n_new, 4) || misaligned(cu, 4) || misaligned(slots, 8)) return BR_EINVAL;
-    const int64_t workers = (int64_t)batch->n_instances * cache->G;
-    if (workers == 0) return BR_OK;
+    if (a.c.workers == 0) return BR_OK;
     a.n_new = n_new; a.room = room; a.cu = cu; a.slots = slots;
-    br::br_slot_map_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, "br_slot_map launch");
-    return BR_OK;
+    const int warps = br::kCacheThreads / 32;
+    if (!n_new)
+        return launch_cache(BR_BY_SLOTS(br_slot_newest_kernel, cache->B), a, warps, 0, batch, "br_slot_map launch");
+    a.c.parts = br::cache_copy_parts(a.c.workers, room);
+    const size_t smem = (size_t)warps * cache->B * (sizeof(br::Run) + sizeof(int));                // at most 24 KB
+    return launch_cache(BR_BY_SLOTS(br_slot_map_kernel, cache->B), a, warps, smem, batch, "br_slot_map launch");
 }
 
 int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
@@ -892,13 +910,12 @@ int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, c
     if (misaligned(n_seq, 4) || misaligned(seq_slot, 4) || misaligned(indptr, 4) || misaligned(indices, 4) ||
         misaligned(last_tokens, 4))
         return BR_EINVAL;
-    const int64_t workers = (int64_t)batch->n_instances * cache->G;
-    if (workers == 0) return BR_OK;
+    if (a.c.workers == 0) return BR_OK;
     a.n_seq = n_seq; a.seq_slot = seq_slot; a.indptr = indptr; a.indices = indices; a.last = last_tokens;
-    br::br_page_lists_kernel<<<(unsigned)workers, br::kCacheThreads, 0, (cudaStream_t)batch->stream>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, "br_page_lists launch");
-    return BR_OK;
+    a.c.parts = br::cache_copy_parts(a.c.workers, cache->pool_blocks);
+    const int warps = br::kCacheThreads / 32;
+    const size_t smem = (size_t)warps * cache->B * sizeof(br::Run);                                // at most 16 KB
+    return launch_cache(BR_BY_SLOTS(br_page_lists_kernel, cache->B), a, warps, smem, batch, "br_page_lists launch");
 }
 
 #ifdef BR_BOUNDS

@@ -48,7 +48,7 @@ def test_library_refuses_bad_arguments_without_touching_the_gpu():
     for n, first in ((-1, 0), (1, -1), (1 << 29, 0), (1, (1 << 29) - 1), ((1 << 31) - 1, (1 << 31) - 1)):
         b = BrInstanceBatch(n_instances=n, first_instance=first, n_steps=1, stream=None)
         assert _calls(b, _cache()) == [BR_EINVAL] * 3, (n, first)
-    for room in (0, -1):
+    for room in (0, -1, (1 << 30) + 1):
         assert _calls(some, _cache(), room=room)[1] == BR_EINVAL
     assert _calls(some, _cache(), a=FAKE, b=FAKE + 4)[1] == BR_EINVAL            # slots are 64-bit
 

@@ -178,6 +178,14 @@ def test_lengths_at_the_ends_of_their_range():
     p.slots(np.full((N, G, B), MOST, np.int32), 7, np.array([3] + [MOST] * 9, np.int32) * np.ones((N, G, 1), np.int32))
 
 
+def test_more_new_tokens_than_31_bits_count():
+    p = Pair(2, 2, 6, 1 << 20, 4100, 2048, seed=8)
+    n = np.array([5, MOST, 7, 9, 3, 1], np.int32) * np.ones((2, 2, 1), np.int32)
+    assert (p.update(n) == 0).all()
+    for q in ([3, MOST, MOST, 9, 1, 1], [MOST, 0, MOST, MOST, MOST, MOST], [0, MOST, 0, 0, 0, 5]):
+        p.slots(n, 41, np.array(q, np.int32) * np.ones((2, 2, 1), np.int32))
+
+
 def test_cache_slots_beyond_32_bits():
     t = 1 << 20
     p = Pair(2, 3, 4, t, 5000, 2048, seed=9)                      # block 4999 starts at slot 5.2e9
