@@ -238,24 +238,28 @@ int cache_args(const br_instance_batch *batch, const br_block_cache *cache, cons
     // (rows are counted in 32 bits; the offsets into the arrays are not)
     if (((int64_t)batch->first_instance + batch->n_instances) * cache->G > 0x7FFFFFFF) return BR_EINVAL;
     c->G = cache->G; c->B = cache->B; c->t = cache->block_tokens; c->T = cache->table_blocks; c->P = cache->pool_blocks;
-    c->first_row = batch->first_instance * cache->G; c->workers = batch->n_instances * cache->G; c->parts = 1;
-    br::cache_divisor(cache->block_tokens, &c->t_magic, &c->t_shift);
+    c->first_row = batch->first_instance * cache->G; c->workers = batch->n_instances * cache->G;
+    c->over_G = br::divisor(cache->G); c->over_t = br::divisor(cache->block_tokens);
     c->len = len; c->step = step;
     c->table = cache->table; c->n_blocks = cache->n_blocks; c->free_list = cache->free_list; c->n_free = cache->n_free;
     return BR_OK;
 }
 
-// Slots per lane of the cache kernels: the smallest power of two that takes B slots with a warp.
-#define BR_BY_SLOTS(kernel, B) ((B) <= 32 ? br::kernel<1> : (B) <= 64 ? br::kernel<2> : (B) <= 128 ? br::kernel<4> : br::kernel<8>)
+template <typename Args>
+struct CacheKernels { void (*one1)(const Args), (*one2)(const Args), (*many1)(const Args), (*many2)(const Args); };
+
+#define BR_CACHE_KERNELS(kernel) {br::kernel<true, 1>, br::kernel<true, 2>, br::kernel<false, 1>, br::kernel<false, 2>}
 
 template <typename Args>
-int launch_cache(void (*kern)(const Args), const Args &a, int warps, size_t smem, const br_instance_batch *batch,
-                        const char *what)
+int launch_cache(const CacheKernels<Args> &k, Args &a, const br::CacheShape &s, const br_instance_batch *batch, const char *what)
 {
-    const int64_t blocks = ((int64_t)a.c.workers * a.c.parts + warps - 1) / warps;
+    const bool one = s.warps == 1;
+    a.c.slices = s.slices; a.c.over_slices = br::divisor(s.slices);
+    const int64_t blocks = one ? ((int64_t)a.c.workers + br::kCacheTeams - 1) / br::kCacheTeams : (int64_t)a.c.workers * s.slices;
     cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
     BR_CUDA(cudaStreamIsCapturing((cudaStream_t)batch->stream, &capturing));
-    cudaError_t e = launch_overlapped(kern, dim3((unsigned)blocks), 32 * warps, smem, (cudaStream_t)batch->stream, a,
+    cudaError_t e = launch_overlapped(one ? (s.spl == 1 ? k.one1 : k.one2) : (s.spl == 1 ? k.many1 : k.many2), dim3((unsigned)blocks),
+                                      32 * (one ? br::kCacheTeams : s.warps), 0, (cudaStream_t)batch->stream, a,
                                       capturing == cudaStreamCaptureStatusNone);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, what);
@@ -876,10 +880,8 @@ int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const
     if (misaligned(n_blocks_out, 4) || misaligned(n_free_out, 4) || misaligned(short_blocks, 4)) return BR_EINVAL;
     if (a.c.workers == 0) return BR_OK;
     a.n_blocks_out = n_blocks_out; a.n_free_out = n_free_out; a.short_out = short_blocks;
-    a.c.parts = br::cache_table_parts(a.c.workers);
-    const int warps = a.c.parts > 1 ? a.c.parts : br::kCacheThreads / 32;
-    const size_t smem = (size_t)(a.c.parts > 1 ? 1 : warps) * 2 * cache->B * sizeof(br::Run);     // at most 32 KB
-    return launch_cache(BR_BY_SLOTS(br_block_tables_kernel, cache->B), a, warps, smem, batch, "br_block_tables launch");
+    const CacheKernels<br::TableArgs> k = BR_CACHE_KERNELS(br_block_tables_kernel);
+    return launch_cache(k, a, br::cache_shape(cache->B, a.c.workers, 1 << 30, 32), batch, "br_block_tables launch");
 }
 
 int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
@@ -892,12 +894,12 @@ int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, con
     if (misaligned(n_new, 4) || misaligned(cu, 4) || misaligned(slots, 8)) return BR_EINVAL;
     if (a.c.workers == 0) return BR_OK;
     a.n_new = n_new; a.room = room; a.cu = cu; a.slots = slots;
-    const int warps = br::kCacheThreads / 32;
-    if (!n_new)
-        return launch_cache(BR_BY_SLOTS(br_slot_newest_kernel, cache->B), a, warps, 0, batch, "br_slot_map launch");
-    a.c.parts = br::cache_copy_parts(a.c.workers, room);
-    const size_t smem = (size_t)warps * cache->B * (sizeof(br::Run) + sizeof(int));                // at most 24 KB
-    return launch_cache(BR_BY_SLOTS(br_slot_map_kernel, cache->B), a, warps, smem, batch, "br_slot_map launch");
+    if (!n_new) {
+        const CacheKernels<br::SlotArgs> k = BR_CACHE_KERNELS(br_slot_newest_kernel);
+        return launch_cache(k, a, br::cache_shape(cache->B, a.c.workers, 1, 8), batch, "br_slot_map launch");
+    }
+    const CacheKernels<br::SlotArgs> k = BR_CACHE_KERNELS(br_slot_map_kernel);
+    return launch_cache(k, a, br::cache_copy_shape(cache->B, a.c.workers, room), batch, "br_slot_map launch");
 }
 
 int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, const int32_t *len, const int32_t *step,
@@ -912,10 +914,8 @@ int br_page_lists(const br_instance_batch *batch, const br_block_cache *cache, c
         return BR_EINVAL;
     if (a.c.workers == 0) return BR_OK;
     a.n_seq = n_seq; a.seq_slot = seq_slot; a.indptr = indptr; a.indices = indices; a.last = last_tokens;
-    a.c.parts = br::cache_copy_parts(a.c.workers, cache->pool_blocks);
-    const int warps = br::kCacheThreads / 32;
-    const size_t smem = (size_t)warps * cache->B * sizeof(br::Run);                                // at most 16 KB
-    return launch_cache(BR_BY_SLOTS(br_page_lists_kernel, cache->B), a, warps, smem, batch, "br_page_lists launch");
+    const CacheKernels<br::PageArgs> k = BR_CACHE_KERNELS(br_page_lists_kernel);
+    return launch_cache(k, a, br::cache_copy_shape(cache->B, a.c.workers, cache->pool_blocks), batch, "br_page_lists launch");
 }
 
 #ifdef BR_BOUNDS
