@@ -13,6 +13,7 @@
 // block otherwise.  Each thread owns one or two slots, and one exchange of the warps' sums gives every slot its place.  What
 // is to be moved is then cut into equal pieces by items, not by slots, so one long request is spread like many short ones.
 #pragma once
+#include <algorithm>
 #include "br_device.cuh"
 #include "../../include/br.h"
 
@@ -76,15 +77,16 @@ inline CacheShape cache_shape(int B, int workers, int pieces, int limit)
     return s;
 }
 
-// a team for copies of up to `items` items a worker, in pieces of 512 or more; more than one block a worker where workers are few
+// A team for copies of up to `items` items a worker.  Several blocks a worker where that fills the GPU with warps of 512 items
+// or more, or evens out the workers' different loads over four rounds of warps of 2,048 or more.
 inline CacheShape cache_copy_shape(int B, int workers, int items)
 {
-    const int pieces = (items + 511) / 512;
-    CacheShape s = cache_shape(B, workers, pieces, 8);
+    CacheShape s = cache_shape(B, workers, (items + 511) / 512, 8);
     if (s.warps > 1) {
-        const long long fill = 2ll * kCacheWarps / ((long long)workers * s.warps), cut = pieces / s.warps;
-        s.slices = (int)(fill < cut ? fill : cut);
-        if (s.slices < 1) s.slices = 1;
+        const long long warps = (long long)workers * s.warps;
+        const long long fill = std::min(kCacheWarps / warps, (long long)items / (512 * s.warps));
+        const long long even = std::min(4 * kCacheWarps / warps, (long long)items / (2048 * s.warps));
+        s.slices = (int)std::max(1ll, std::max(fill, even));
     }
     return s;
 }
@@ -125,6 +127,7 @@ struct Seat {
         }
         row = (size_t)c.first_row + worker;
     }
+    __device__ __forceinline__ bool first_block() const { return ONE || piece < (int)(blockDim.x >> 5); }   // of its worker's
     __device__ __forceinline__ int step(const CacheArgs &c) const { return c.step ? c.step[over((int)row, c.over_G)] : 0; }
 };
 
@@ -148,9 +151,9 @@ __device__ __forceinline__ int lanes_below(int v, int lane)
 template <bool ONE>
 __device__ __forceinline__ TeamSums team_sums(int x, int y, int z, int4 *part, int lane, int warp)
 {
-    TeamSums s;
-    s.x = lanes_below(x, lane); s.y = lanes_below(y, lane);
-    s.x_all = __shfl_sync(kFull, add_to_most(s.x, x), 31); s.y_all = __shfl_sync(kFull, s.y + y, 31);
+    TeamSums s = {0, 0, 0, 0, 0};
+    if (__any_sync(kFull, x != 0)) { s.x = lanes_below(x, lane); s.x_all = __shfl_sync(kFull, add_to_most(s.x, x), 31); }
+    if (__any_sync(kFull, y != 0)) { s.y = lanes_below(y, lane); s.y_all = __shfl_sync(kFull, s.y + y, 31); }
     s.z_all = (int)__reduce_add_sync(kFull, (unsigned)z);
     if (ONE) return s;
     if (lane == 0) part[warp] = make_int4(s.x_all, s.y_all, s.z_all, 0);
@@ -168,31 +171,127 @@ __device__ __forceinline__ TeamSums team_sums(int x, int y, int z, int4 *part, i
     return s;
 }
 
-// A slot's run of items in the sequence of all items of its worker: item e of the run, e < upto, is at e + shift in the slot.
+// A slot's run of items in the sequence of all items of its worker: item e of the run, e < upto, is entry e + shift of the
+// worker's table (at most 256 rows of 2^22: the sum fits 32 bits).
 struct Run { int upto, shift; };
+// ... or token e + shift of the slot whose row is at `base` and holds `held` blocks
+struct alignas(16) TokenRun { int upto, shift, base, held; };
 
-// Position in the runs of a worker's B slots.
+// Position in a worker's runs.
+template <typename RunT>
 struct Walk {
-    const Run *runs;
-    int B, slot;
-    Run at;
-    // the slot of item e: the first whose run ends behind it
-    __device__ __forceinline__ void seek(const Run *r, int B_, int e)
+    const RunT *runs;
+    int last, here;
+    RunT at;
+    // the run of item e: the first that ends behind it (e lies in one of them)
+    __device__ __forceinline__ void seek(const RunT *r, int count, int e)
     {
-        runs = r; B = B_;
-        int lo = 0, hi = B - 1;
+        runs = r; last = count - 1;
+        int lo = 0, hi = last;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
             if (runs[mid].upto > e) hi = mid; else lo = mid + 1;
         }
-        slot = lo; at = runs[lo];
+        here = lo; at = runs[lo];
     }
     // on to item e, not before the present one
     __device__ __forceinline__ void to(int e)
     {
-        while (at.upto <= e && slot < B - 1) at = runs[++slot];
+        while (at.upto <= e && here < last) at = runs[++here];
     }
 };
+
+// A list whose entry -x is out[x].
+template <typename Out> struct UpList {
+    Out out;
+    __device__ __forceinline__ auto &operator[](int i) const { return out[-i]; }
+};
+
+// The runs of the items of one warp, window by window of kMoves rows of 32: a bit for each item that starts a run turns into
+// the run of every item by counting bits, which has no loop that lanes leave one by one.  No run is empty.
+struct Windows {
+    const Run *runs;
+    int n, run;                             // run: that of the window's first item
+    __device__ __forceinline__ void seek(const Run *r, int count, int e, int lane)
+    {
+        runs = r; n = count; run = 0;
+        for (int k = 0; k < n; k += 32) run += __popc(__ballot_sync(kFull, k + lane < n && runs[k + lane].upto <= e));
+    }
+    // shift[u] of item e0 + 32 u + lane; on to the next window.  True if one run covers the window.
+    __device__ __forceinline__ bool next(int e0, int lane, int (&shift)[kMoves])
+    {
+        int d = run + lane < n - 1 ? runs[run + lane].upto - e0 : 1 << 30;      // run + lane + 1 starts d items into the window
+        unsigned in = __ballot_sync(kFull, d <= 32 * kMoves);
+        const int only = runs[run].shift;
+#pragma unroll
+        for (int u = 0; u < kMoves; ++u) shift[u] = only;
+        if (in == 0) return true;
+        int count = __popc(in);
+        if (count == 1) {
+            const int from = __shfl_sync(kFull, d, 0) - lane, then = runs[++run].shift;
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u) shift[u] = 32 * u >= from ? then : only;
+            return false;
+        }
+        unsigned starts[kMoves];
+#pragma unroll
+        for (int u = 0; u < kMoves; ++u) starts[u] = 0;
+        for (int k = run + lane;;) {
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u) starts[u] |= __reduce_or_sync(kFull, (d >> 5) == u ? 1u << (d & 31) : 0u);
+            if (in != kFull) break;
+            k += 32;
+            d = k < n - 1 ? runs[k].upto - e0 : 1 << 30;
+            in = __ballot_sync(kFull, d <= 32 * kMoves);
+            count += __popc(in);
+        }
+        int r = run;
+#pragma unroll
+        for (int u = 0; u < kMoves; ++u) {
+            shift[u] = runs[r + __popc(starts[u] & (0xFFFFFFFFu >> (31 - lane)))].shift;
+            r += __popc(starts[u]);
+        }
+        run += count;
+        return false;
+    }
+};
+
+// Moves items [lo, hi) of a warp, kMoves of a lane at a time: item x is entry x + shift of its run in `table`, or entry top - x
+// of `list`.
+template <bool FROM_TABLE, bool TO_TABLE, typename Table, typename List>
+__device__ __forceinline__ void move_items(const Run *from_runs, int n_from, const Run *to_runs, int n_to, int lo, int hi, int lane,
+                                           const Table &table, const List &list, int top)
+{
+    if (lo >= hi) return;
+    Windows from, to;
+    if (FROM_TABLE) from.seek(from_runs, n_from, lo, lane);
+    if (TO_TABLE) to.seek(to_runs, n_to, lo, lane);
+    for (int e0 = lo; e0 < hi; e0 += 32 * kMoves) {
+        const int e = e0 + lane;
+        const bool full = e0 + 32 * kMoves <= hi;
+        int id[kMoves], shift[kMoves];
+        const bool one = FROM_TABLE ? from.next(e0, lane, shift) : true;
+        if (full && one) {
+            const int entry = FROM_TABLE ? e + shift[0] : top - e;
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u) id[u] = FROM_TABLE ? table[entry + 32 * u] : list[entry - 32 * u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u)
+                if (e + 32 * u < hi) id[u] = FROM_TABLE ? table[e + 32 * u + shift[u]] : list[top - e - 32 * u];
+        }
+        const bool one_to = TO_TABLE ? to.next(e0, lane, shift) : true;
+        if (full && one_to) {
+            const int entry = TO_TABLE ? e + shift[0] : top - e;
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u) (TO_TABLE ? table[entry + 32 * u] : list[entry - 32 * u]) = id[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < kMoves; ++u)
+                if (e + 32 * u < hi) (TO_TABLE ? table[e + 32 * u + shift[u]] : list[top - e - 32 * u]) = id[u];
+        }
+    }
+}
 
 // Items [lo, hi) of `count` for one of `pieces`: equal numbers of units of 128, counted from `skew` items ahead of the first.
 __device__ __forceinline__ void cache_piece(int piece, int pieces, int count, int skew, int *lo, int *hi)
@@ -208,12 +307,13 @@ __device__ __forceinline__ void cache_piece(int piece, int pieces, int count, in
 // rows that shrink, the list below n_free) is never written by the same call, so the moves need no order.  The counts may be
 // written where they are read: a slot's by the thread that read it, the worker's after the whole team has read them.
 template <bool ONE, int SPL>
-__global__ void __launch_bounds__(ONE ? 32 * kCacheTeams : 1024) br_block_tables_kernel(const TableArgs a)
+__global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs a)
 {
     constexpr int kSlots = ONE ? 32 * SPL : BR_MAX_B;
     __shared__ Run runs[ONE ? kCacheTeams : 1][2][kSlots];
-    __shared__ int4 part[ONE ? 1 : 32];
+    __shared__ int4 part[ONE ? 1 : 8];
     __shared__ int granted[ONE ? 1 : 8];
+    __shared__ int2 ranks[ONE ? 1 : 8];
     __shared__ long long lacks[ONE ? 1 : 8];
     stream_order_gate();
     const CacheArgs &c = a.c;
@@ -255,18 +355,69 @@ __global__ void __launch_bounds__(ONE ? 32 * kCacheTeams : 1024) br_block_tables
         return;
     }
     const int R = sum.x_all;
+    // between two decode steps most workers only grow, by a block a request at most, and all of it fits: each thread serves
+    // its own slots
+    if (ONE && R == 0 && sum.y_all <= n_free) {
+        bool single = true;
+#pragma unroll
+        for (int i = 0; i < SPL; ++i) single = single && need[i] <= have[i] + 1;
+        if (__all_sync(kFull, single)) {
+            const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
+            const auto list = mk_span(c.free_list + row * c.P, c.P);
+            int id[SPL], lacking = 0;
+#pragma unroll
+            for (int i = 0; i < SPL; ++i) {
+                id[i] = -1;
+                if (need[i] > have[i]) {
+                    if (need[i] <= c.T) id[i] = list[n_free - 1 - sum.y++]; else ++lacking;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < SPL; ++i) {
+                if (at.slot + i >= c.B) break;
+                const bool more = need[i] > have[i] && need[i] <= c.T;
+                if (more) table[(at.slot + i) * c.T + have[i]] = id[i];
+                a.n_blocks_out[slots + at.slot + i] = have[i] + more;
+            }
+            lacking = (int)__reduce_add_sync(kFull, (unsigned)lacking);
+            if (at.lane == 0) {
+                a.n_free_out[row] = n_free - sum.y_all;
+                if (a.short_out) a.short_out[row] = lacking;
+            }
+            return;
+        }
+    }
+    // the slots that give blocks back, and those that ask for some, are packed: few of them do either between two steps
+    int back_rank = 0, grow_rank = 0, runs_back = 0, runs_grow = 0;
+    const unsigned below = (1u << at.lane) - 1;
+#pragma unroll
+    for (int i = 0; i < SPL; ++i) {
+        const unsigned backs = __ballot_sync(kFull, have[i] > need[i]), grows = __ballot_sync(kFull, need[i] > have[i] && need[i] <= c.T);
+        back_rank += __popc(backs & below); grow_rank += __popc(grows & below);
+        runs_back += __popc(backs); runs_grow += __popc(grows);
+    }
+    if (!ONE) {
+        if (at.lane == 0 && at.warp < 8) ranks[at.warp] = make_int2(runs_back, runs_grow);
+        __syncthreads();
+        runs_back = runs_grow = 0;
+        for (int w = 0; w < min((int)(blockDim.x >> 5), 8); ++w) {
+            const int2 r = ranks[w];
+            if (w < at.warp) { back_rank += r.x; grow_rank += r.y; }
+            runs_back += r.x; runs_grow += r.y;
+        }
+    }
     int A = 0;
     long long lacking = 0;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         if (at.slot + i >= c.B) break;
         const int less = max(have[i] - need[i], 0), more = max(need[i] - have[i], 0);
-        back_run[at.slot + i] = {sum.x + less, need[i] - sum.x};
+        if (less > 0) back_run[back_rank++] = {sum.x + less, (at.slot + i) * c.T + need[i] - sum.x};
         sum.x += less;
         // a sum over all demands up to this one: the first that does not fit keeps out the ones behind it
         const int upto = sum.y + (need[i] <= c.T ? more : 0);
         const bool fits = need[i] <= c.T && upto <= n_free + R;
-        grow_run[at.slot + i] = {fits ? upto : sum.y, have[i] - sum.y};
+        if (more > 0 && need[i] <= c.T) grow_run[grow_rank++] = {fits ? upto : sum.y, (at.slot + i) * c.T + have[i] - sum.y};
         sum.y = upto;
         if (fits) A = upto; else lacking += more;
         a.n_blocks_out[slots + at.slot + i] = have[i] + (fits ? more : 0) - less;
@@ -286,38 +437,21 @@ __global__ void __launch_bounds__(ONE ? 32 * kCacheTeams : 1024) br_block_tables
     }
     int lo, hi;
     cache_piece(at.piece, at.pieces, max(R, A), 0, &lo, &hi);
-    int e = lo + at.lane;
-    if (e >= hi) return;
     const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
     const auto list = mk_span(c.free_list + row * c.P, c.P);
-    Walk from, to;
-    if (e < R) from.seek(back_run, c.B, e);
-    if (e < A) to.seek(grow_run, c.B, e);
-    for (; e < hi; e += 32 * kMoves) {
-        int id[kMoves];
-#pragma unroll
-        for (int u = 0; u < kMoves; ++u) {
-            const int x = e + 32 * u;
-            if (x >= hi) break;
-            if (x < R) {
-                from.to(x);
-                id[u] = table[(long long)from.slot * c.T + x + from.at.shift];
-            } else {
-                id[u] = list[n_free + R - 1 - x];
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kMoves; ++u) {
-            const int x = e + 32 * u;
-            if (x >= hi) break;
-            if (x < A) {
-                to.to(x);
-                table[(long long)to.slot * c.T + x + to.at.shift] = id[u];
-            } else {
-                list[n_free + R - 1 - x] = id[u];
-            }
-        }
-    }
+    const int both = min(R, A), top = n_free + R - 1;
+    move_items<true, true>(back_run, runs_back, grow_run, runs_grow, lo, min(hi, both), at.lane, table, list, top);
+    lo = max(lo, both);
+    if (R < A) move_items<false, true>(back_run, 0, grow_run, runs_grow, lo, hi, at.lane, table, list, top);
+    else move_items<true, false>(back_run, runs_back, grow_run, 0, lo, hi, at.lane, table, list, top);
+}
+
+// An entry with no other one of interest near it: 64 bytes of memory are fetched for it, not the usual 128.
+__device__ __forceinline__ int lone_entry(const int32_t *p)
+{
+    int v;
+    asm volatile("ld.global.L2::64B.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
 }
 
 // One new token a request.
@@ -348,7 +482,7 @@ __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
         if (n[i] > 0) {
             const int column = over(n[i] - 1, c.over_t);
             if (column < min(held[i], c.T))
-                slot[i] = (long long)table[(long long)(at.slot + i) * c.T + column] * c.t + (n[i] - 1 - column * c.t);
+                slot[i] = (long long)lone_entry(&table[(at.slot + i) * c.T + column]) * c.t + (n[i] - 1 - column * c.t);
             ++count;
         }
     }
@@ -380,15 +514,13 @@ template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
 {
     constexpr int kSlots = ONE ? 32 * SPL : BR_MAX_B;
-    __shared__ Run runs[ONE ? kCacheTeams : 1][kSlots];
-    __shared__ int held_by[ONE ? kCacheTeams : 1][kSlots];
+    __shared__ TokenRun runs[ONE ? kCacheTeams : 1][kSlots];
     __shared__ int4 part[ONE ? 1 : 8];
     stream_order_gate();
     const CacheArgs &c = a.c;
     const Seat<ONE, SPL> at(c);
     if (!at.any) return;
-    Run *run = runs[ONE ? at.warp : 0];
-    int *held_of = held_by[ONE ? at.warp : 0];
+    TokenRun *run = runs[ONE ? at.warp : 0];
     const size_t row = at.row, slots = row * c.B;
     const int step = at.step(c);
     int n[SPL], q[SPL], held[SPL], mine = 0;
@@ -409,7 +541,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     }
     const TeamSums sum = team_sums<ONE>(mine, 0, 0, part, at.lane, at.warp);
     const auto cu = mk_span(a.cu + row * (c.B + 1), c.B + 1);
-    const bool first_slice = at.piece < (ONE ? 1 : (int)(blockDim.x >> 5));
+    const bool first_block = at.first_block();
     int place = sum.x;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
@@ -417,9 +549,9 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
         if (b >= c.B) break;
         const int from = place;
         place = add_to_most(place, q[i]);
-        run[b] = {place, n[i] - q[i] - from};         // (a run that starts at 2^31 - 1 has no item below `room`)
-        held_of[b] = min(max(held[i], 0), c.T);
-        if (first_slice) {
+        // (a run that starts at 2^31 - 1 has no item below `room`)
+        run[b] = {place, n[i] - q[i] - from, b * c.T, min(max(held[i], 0), c.T)};
+        if (first_block) {
             cu[b] = from;
             if (b == c.B - 1) cu[c.B] = place;
         }
@@ -432,41 +564,42 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     const int skew = (int)(reinterpret_cast<uintptr_t>(a.slots + row * a.room) >> 3) & 3;
     int lo, hi;
     cache_piece(at.piece, at.pieces, count, skew, &lo, &hi);
-    int e = (lo + skew) / 128 * 128 + 4 * at.lane - skew;          // (lo is at a unit's start, or the row's)
+    int e = (lo + skew) / 128 * 128 - skew + 4 * at.lane;     // (lo is at a unit's start, or the row's)
     if (max(e, lo) >= hi) return;
-    Walk w;
+    Walk<TokenRun> w;
     w.seek(run, c.B, max(e, lo));
     for (; e < hi; e += 128) {
-        const int first = max(e, lo);
-        w.to(first);
-        if (e >= lo && e + 4 <= min(hi, w.at.upto) && c.t >= 4) {
-            const int p = e + w.at.shift, column = over(p, c.over_t), off = p - column * c.t, held_here = held_of[w.slot];
-            const long long entry = (long long)w.slot * c.T + column;
-            const bool next = off + 3 >= c.t;
-            const long long id0 = column < held_here ? table[entry] : -1, id1 = next && column + 1 < held_here ? table[entry + 1] : -1;
-            const long long s0 = id0 * c.t + off, s1 = id1 * c.t + off - c.t;
+        w.to(max(e, lo));
+        const int p = e + w.at.shift, column = over(max(p, 0), c.over_t), offset = p - column * c.t;
+        const bool next = offset + 3 >= c.t;
+        if (e >= lo && e + 4 <= min(hi, w.at.upto) && c.t >= 4 && column + next < w.at.held) {
+            // four tokens of one request, in one block or two
+            const int entry = w.at.base + column, id0 = table[entry], id1 = next ? table[entry + 1] : 0;
+            const long long s0 = (long long)id0 * c.t + offset, s1 = (long long)id1 * c.t + (offset - c.t);
             FourSlots v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool in0 = off + j < c.t;
-                v.v[j] = (in0 ? column : column + 1) < held_here ? (in0 ? s0 : s1) + j : -1;
-            }
+            for (int j = 0; j < 4; ++j) v.v[j] = (offset + j < c.t ? s0 : s1) + j;
             store_four(vec_at<FourSlots>(out, e), v);
         } else {
-            const int last = min(e + 4, hi);
-            for (int x = first; x < last; ++x) {
-                w.to(x);
-                const int p = x + w.at.shift, column = over(p, c.over_t);
-                out[x] = column < held_of[w.slot]
-                             ? (long long)table[(long long)w.slot * c.T + column] * c.t + (p - column * c.t) : -1;
+            int id[4], off[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                id[j] = off[j] = -1;
+                if (e + j < lo || e + j >= hi) continue;
+                w.to(e + j);
+                const int pj = e + j + w.at.shift, cj = over(pj, c.over_t);
+                if (cj < w.at.held) { off[j] = pj - cj * c.t; id[j] = table[w.at.base + cj]; }
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j >= lo && e + j < hi) out[e + j] = off[j] < 0 ? -1 : (long long)id[j] * c.t + off[j];
         }
     }
 }
 
 // The running slots move up, their blocks follow one another.
 template <bool ONE, int SPL>
-__global__ void __launch_bounds__(256) br_page_lists_kernel(const PageArgs a)
+__global__ void __launch_bounds__(256, 6) br_page_lists_kernel(const PageArgs a)
 {
     constexpr int kSlots = ONE ? 32 * SPL : BR_MAX_B;
     __shared__ Run runs[ONE ? kCacheTeams : 1][kSlots];
@@ -478,7 +611,7 @@ __global__ void __launch_bounds__(256) br_page_lists_kernel(const PageArgs a)
     Run *run = runs[ONE ? at.warp : 0];
     const size_t row = at.row, slots = row * c.B;
     const int step = at.step(c);
-    int n[SPL], held[SPL], mine = 0, running = 0;
+    int n[SPL], held[SPL], mine = 0, counts = 0;             // counts: running requests, and those with blocks 16 bits up
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         n[i] = BR_EMPTY_SLOT; held[i] = 0;
@@ -488,52 +621,39 @@ __global__ void __launch_bounds__(256) br_page_lists_kernel(const PageArgs a)
     for (int i = 0; i < SPL; ++i) {
         n[i] = cache_tokens(n[i], step);
         held[i] = min(max(held[i], 0), c.T);
-        mine += min(cache_blocks(c, n[i]), held[i]);
-        running += n[i] > 0;
+        const int pages = min(cache_blocks(c, n[i]), held[i]);
+        mine += pages;
+        counts += (n[i] > 0) + ((pages > 0) << 16);
     }
-    const TeamSums sum = team_sums<ONE>(mine, running, 0, part, at.lane, at.warp);
+    const TeamSums sum = team_sums<ONE>(mine, counts, 0, part, at.lane, at.warp);
     const auto seq_slot = mk_span(a.seq_slot + slots, c.B), last = mk_span(a.last + slots, c.B);
     const auto indptr = mk_span(a.indptr + row * (c.B + 1), c.B + 1);
-    const bool first_slice = at.piece < (ONE ? 1 : (int)(blockDim.x >> 5));
-    int place = sum.x, rank = sum.y;
+    const bool first_block = at.first_block();
+    const int n_seq = sum.y_all & 0xFFFF, runs_all = sum.y_all >> 16;
+    int place = sum.x, rank = sum.y & 0xFFFF, run_rank = sum.y >> 16;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         const int b = at.slot + i;
         if (b >= c.B) break;
         const int need = cache_blocks(c, n[i]), pages = min(need, held[i]);
-        if (first_slice && n[i] > 0) {
+        if (first_block && n[i] > 0) {
             seq_slot[rank] = b;
             indptr[rank] = place;
             last[rank] = pages == 0 ? 0 : need <= held[i] ? n[i] - (need - 1) * c.t : c.t;
             ++rank;
         }
-        run[b] = {place + pages, -place};
+        if (pages > 0) run[run_rank++] = {place + pages, b * c.T - place};
         place += pages;
-        if (first_slice && b >= sum.y_all) { seq_slot[b] = -1; last[b] = 0; indptr[b] = sum.x_all; }
+        if (first_block && b >= n_seq) { seq_slot[b] = -1; last[b] = 0; indptr[b] = sum.x_all; }
     }
-    if (first_slice && at.slot == 0) { indptr[c.B] = sum.x_all; a.n_seq[row] = sum.y_all; }
+    if (first_block && at.slot == 0) { indptr[c.B] = sum.x_all; a.n_seq[row] = n_seq; }
     team_sync<ONE>();
     const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
     const auto out = mk_span(a.indices + row * c.P, c.P);
     int lo, hi;
     cache_piece(at.piece, at.pieces, min(sum.x_all, c.P), 0, &lo, &hi);
-    int e = lo + at.lane;
-    if (e >= hi) return;
-    Walk w;
-    w.seek(run, c.B, e);
-    for (; e < hi; e += 32 * kMoves) {
-        int id[kMoves];
-#pragma unroll
-        for (int u = 0; u < kMoves; ++u) {
-            const int x = e + 32 * u;
-            if (x >= hi) break;
-            w.to(x);
-            id[u] = table[(long long)w.slot * c.T + x + w.at.shift];
-        }
-#pragma unroll
-        for (int u = 0; u < kMoves; ++u)
-            if (e + 32 * u < hi) out[e + 32 * u] = id[u];
-    }
+    // (indices are a list that runs upwards: entry x of it is item x)
+    move_items<true, false>(run, runs_all, run, 0, lo, hi, at.lane, table, UpList<decltype(out)>{out}, 0);
 }
 
 }  // namespace br
