@@ -91,18 +91,18 @@ inline CacheShape cache_copy_shape(int B, int workers, int items)
     return s;
 }
 
-// tokens of the request in a slot: len + step, at least 0 and at most 2^31 - 1; 0 for a free slot
-__device__ __forceinline__ int cache_tokens(int len, int step)
+// a + b, at most 2^31 - 1 and at least -2^31
+__device__ __forceinline__ int add_to_most(int a, int b)
 {
-    if (len == BR_EMPTY_SLOT) return 0;
-    const long long n = (long long)len + step;
-    return n < 0 ? 0 : n > 0x7FFFFFFF ? 0x7FFFFFFF : (int)n;
+    int s;
+    asm("add.sat.s32 %0, %1, %2;" : "=r"(s) : "r"(a), "r"(b));
+    return s;
 }
 
-__device__ __forceinline__ int cache_blocks(const CacheArgs &c, int tokens) { return tokens > 0 ? over(tokens - 1, c.over_t) + 1 : 0; }
+// tokens of the request in a slot: len + step, at least 0 and at most 2^31 - 1; 0 for a free slot
+__device__ __forceinline__ int cache_tokens(int len, int step) { return len == BR_EMPTY_SLOT ? 0 : max(add_to_most(len, step), 0); }
 
-// a + b for 0 <= a, b < 2^31, at most 2^31 - 1
-__device__ __forceinline__ int add_to_most(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7FFFFFFFu); }
+__device__ __forceinline__ int cache_blocks(const CacheArgs &c, int tokens) { return tokens > 0 ? over(tokens - 1, c.over_t) + 1 : 0; }
 
 // One thread's place: its team's worker, its first slot, and the piece of the worker's items that its warp moves.
 template <bool ONE, int SPL>
@@ -133,41 +133,51 @@ struct Seat {
 
 template <bool ONE> __device__ __forceinline__ void team_sync() { if (ONE) __syncwarp(); else __syncthreads(); }
 
-// Sums over the threads of the team below this one, and over all: of x (at most 2^31 - 1 each) and y, and the sum of z.
-struct TeamSums { int x, y, x_all, y_all, z_all; };
+// Sums over the threads of the team below this one, and over all of them, of x (at most 2^31 - 1 each) and y; the sum of z; and
+// of w, a warp's own, the sums over the warps below and over all.
+struct TeamSums { int x, y, x_all, y_all, z_all, w, w_all; };
 
-__device__ __forceinline__ int lanes_below(int v, int lane)
+// sum over the lanes below; *all: over the warp
+__device__ __forceinline__ int lanes_below(int v, int lane, int *all)
 {
     int in = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(kFull, in, o);
-        if (lane >= o) in = add_to_most(in, u);
-    }
+    for (int o = 1; o < 32; o <<= 1)
+        // (the shuffle's predicate says whether the lane o below is there)
+        asm volatile("{ .reg .pred p; .reg .b32 u; shfl.sync.up.b32 u|p, %0, %1, 0, 0xffffffff; @p add.sat.s32 %0, %0, u; }" : "+r"(in) : "r"(o));
+    *all = __shfl_sync(kFull, in, 31);
     const int below = __shfl_up_sync(kFull, in, 1);
     return lane ? below : 0;
 }
 
-template <bool ONE>
-__device__ __forceinline__ TeamSums team_sums(int x, int y, int z, int4 *part, int lane, int warp)
+// MOST: sums of x may pass 2^31 - 1.
+template <bool ONE, bool MOST>
+__device__ __forceinline__ TeamSums team_sums(int x, int y, int z, int w, int4 *part, int lane, int warp)
 {
-    TeamSums s = {0, 0, 0, 0, 0};
-    if (__any_sync(kFull, x != 0)) { s.x = lanes_below(x, lane); s.x_all = __shfl_sync(kFull, add_to_most(s.x, x), 31); }
-    if (__any_sync(kFull, y != 0)) { s.y = lanes_below(y, lane); s.y_all = __shfl_sync(kFull, s.y + y, 31); }
+    TeamSums s = {0, 0, 0, 0, 0, 0, w};
+    if (__any_sync(kFull, x != 0)) s.x = lanes_below(x, lane, &s.x_all);
+    if (__any_sync(kFull, y != 0)) s.y = lanes_below(y, lane, &s.y_all);
     s.z_all = (int)__reduce_add_sync(kFull, (unsigned)z);
     if (ONE) return s;
-    if (lane == 0) part[warp] = make_int4(s.x_all, s.y_all, s.z_all, 0);
+    if (lane == 0) part[warp] = make_int4(s.x_all, s.y_all, s.z_all, w);
     __syncthreads();
-    // (slots end with the eighth warp: 256 of them, one a thread)
-    s.x_all = s.y_all = s.z_all = 0;
-    const int warps = min((int)(blockDim.x >> 5), 8);
-    int xb = 0, yb = 0;
-    for (int w = 0; w < warps; ++w) {
-        const int4 p = part[w];
-        if (w == warp) { xb = s.x_all; yb = s.y_all; }
-        s.x_all = add_to_most(s.x_all, p.x); s.y_all += p.y; s.z_all += p.z;
+    // (at most eight warps; lane l takes the sums of warp l)
+    const int4 p = lane < (int)(blockDim.x >> 5) ? part[lane] : make_int4(0, 0, 0, 0);
+    const bool below = lane < warp;
+    if (MOST) {                             // (the high and the low half apart, then at most 2^31 - 1)
+        const unsigned hi = __reduce_add_sync(kFull, (unsigned)p.x >> 16), lo = __reduce_add_sync(kFull, p.x & 0xFFFFu);
+        const unsigned hb = __reduce_add_sync(kFull, below ? (unsigned)p.x >> 16 : 0u), lb = __reduce_add_sync(kFull, below ? p.x & 0xFFFFu : 0u);
+        s.x_all = (int)min(((unsigned long long)hi << 16) + lo, 0x7FFFFFFFull);
+        s.x = add_to_most(s.x, (int)min(((unsigned long long)hb << 16) + lb, 0x7FFFFFFFull));
+    } else {
+        s.x_all = (int)__reduce_add_sync(kFull, (unsigned)p.x);
+        s.x += (int)__reduce_add_sync(kFull, below ? (unsigned)p.x : 0u);
     }
-    s.x = add_to_most(s.x, xb); s.y += yb;
+    s.y_all = (int)__reduce_add_sync(kFull, (unsigned)p.y);
+    s.y += (int)__reduce_add_sync(kFull, below ? (unsigned)p.y : 0u);
+    s.z_all = (int)__reduce_add_sync(kFull, (unsigned)p.z);
+    s.w_all = (int)__reduce_add_sync(kFull, (unsigned)p.w);
+    s.w = (int)__reduce_add_sync(kFull, below ? (unsigned)p.w : 0u);
     return s;
 }
 
@@ -313,37 +323,45 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
     __shared__ Run runs[ONE ? kCacheTeams : 1][2][kSlots];
     __shared__ int4 part[ONE ? 1 : 8];
     __shared__ int granted[ONE ? 1 : 8];
-    __shared__ int2 ranks[ONE ? 1 : 8];
-    __shared__ long long lacks[ONE ? 1 : 8];
+    __shared__ long long wanted[ONE ? 1 : 8];
     stream_order_gate();
     const CacheArgs &c = a.c;
     const Seat<ONE, SPL> at(c);
     if (!at.any) return;
-    Run *back_run = runs[ONE ? at.warp : 0][0], *grow_run = runs[ONE ? at.warp : 0][1];
     const size_t row = at.row, slots = row * c.B;
     const int step = at.step(c), n_free = c.n_free[row];
     int need[SPL], have[SPL], held = 0, back = 0, ask = 0;
-    bool bad = (unsigned)n_free > (unsigned)c.P;
+    bool bad = false, too_long = false, several = false;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         need[i] = BR_EMPTY_SLOT; have[i] = 0;
         if (at.slot + i < c.B) { need[i] = c.len[slots + at.slot + i]; have[i] = c.n_blocks[slots + at.slot + i]; }
     }
+    // the slots that give blocks back, and those that ask for some, are counted: their runs are packed
+    int back_rank = 0, grow_rank = 0, n_back = 0, n_grow = 0;
+    const unsigned below = (1u << at.lane) - 1;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         need[i] = cache_blocks(c, cache_tokens(need[i], step));
-        if ((unsigned)have[i] > (unsigned)c.T) { bad = true; continue; }
-        held += have[i];
-        back += max(have[i] - need[i], 0);
-        ask += need[i] <= c.T ? max(need[i] - have[i], 0) : 0;
+        const bool in_range = (unsigned)have[i] <= (unsigned)c.T, fits_row = need[i] <= c.T;
+        const int more = in_range ? need[i] - have[i] : 0;
+        bad = bad || !in_range;
+        too_long = too_long || !fits_row;
+        several = several || more > 1;
+        held += in_range ? have[i] : 0;
+        back += max(-more, 0);
+        ask += fits_row ? max(more, 0) : 0;
+        const unsigned backs = __ballot_sync(kFull, more < 0), grows = __ballot_sync(kFull, more > 0 && fits_row);
+        back_rank += __popc(backs & below); grow_rank += __popc(grows & below);
+        n_back += __popc(backs); n_grow += __popc(grows);
     }
-    // (with counts in range all sums stay below 2^30)
-    bad = ONE ? __any_sync(kFull, bad) : __syncthreads_or(bad);
-    TeamSums sum = {0, 0, 0, 0, 0};
-    if (!bad) {
-        sum = team_sums<ONE>(back, ask, held, part, at.lane, at.warp);
-        bad = n_free + sum.z_all > c.P;
-    }
+    const int flags = (__any_sync(kFull, bad) ? 1 << 20 : 0) + (__any_sync(kFull, too_long) ? 1 << 24 : 0) +
+                      (__any_sync(kFull, several) ? 1 << 28 : 0);
+    // (with counts in range all sums stay below 2^30; counts and flags take ten and four bits, from eight warps)
+    TeamSums sum = team_sums<ONE, false>(back, ask, held, n_back + (n_grow << 10) + flags, part, at.lane, at.warp);
+    n_back = sum.w_all & 1023; n_grow = sum.w_all >> 10 & 1023;
+    bad = (sum.w_all & 15 << 20) != 0 || (unsigned)n_free > (unsigned)c.P || n_free + sum.z_all > c.P;
+    too_long = (sum.w_all & 15 << 24) != 0; several = ((unsigned)sum.w_all >> 28) != 0;
     if (bad) {                              // counts that no sequence of updates leaves behind: the worker stays as it is
 #pragma unroll
         for (int i = 0; i < SPL; ++i)
@@ -355,59 +373,31 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
         return;
     }
     const int R = sum.x_all;
+    const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
+    const auto list = mk_span(c.free_list + row * c.P, c.P);
+    const bool all_fit = !too_long && sum.y_all <= n_free + R;
     // between two decode steps most workers only grow, by a block a request at most, and all of it fits: each thread serves
     // its own slots
-    if (ONE && R == 0 && sum.y_all <= n_free) {
-        bool single = true;
+    if (R == 0 && all_fit && !several) {
+        int id[SPL];
 #pragma unroll
-        for (int i = 0; i < SPL; ++i) single = single && need[i] <= have[i] + 1;
-        if (__all_sync(kFull, single)) {
-            const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
-            const auto list = mk_span(c.free_list + row * c.P, c.P);
-            int id[SPL], lacking = 0;
+        for (int i = 0; i < SPL; ++i) id[i] = need[i] > have[i] ? list[n_free - 1 - sum.y++] : -1;
 #pragma unroll
-            for (int i = 0; i < SPL; ++i) {
-                id[i] = -1;
-                if (need[i] > have[i]) {
-                    if (need[i] <= c.T) id[i] = list[n_free - 1 - sum.y++]; else ++lacking;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < SPL; ++i) {
-                if (at.slot + i >= c.B) break;
-                const bool more = need[i] > have[i] && need[i] <= c.T;
-                if (more) table[(at.slot + i) * c.T + have[i]] = id[i];
-                a.n_blocks_out[slots + at.slot + i] = have[i] + more;
-            }
-            lacking = (int)__reduce_add_sync(kFull, (unsigned)lacking);
-            if (at.lane == 0) {
-                a.n_free_out[row] = n_free - sum.y_all;
-                if (a.short_out) a.short_out[row] = lacking;
-            }
-            return;
+        for (int i = 0; i < SPL; ++i) {
+            if (at.slot + i >= c.B) break;
+            if (need[i] > have[i]) table[(at.slot + i) * c.T + have[i]] = id[i];
+            a.n_blocks_out[slots + at.slot + i] = need[i];
         }
-    }
-    // the slots that give blocks back, and those that ask for some, are packed: few of them do either between two steps
-    int back_rank = 0, grow_rank = 0, runs_back = 0, runs_grow = 0;
-    const unsigned below = (1u << at.lane) - 1;
-#pragma unroll
-    for (int i = 0; i < SPL; ++i) {
-        const unsigned backs = __ballot_sync(kFull, have[i] > need[i]), grows = __ballot_sync(kFull, need[i] > have[i] && need[i] <= c.T);
-        back_rank += __popc(backs & below); grow_rank += __popc(grows & below);
-        runs_back += __popc(backs); runs_grow += __popc(grows);
-    }
-    if (!ONE) {
-        if (at.lane == 0 && at.warp < 8) ranks[at.warp] = make_int2(runs_back, runs_grow);
-        __syncthreads();
-        runs_back = runs_grow = 0;
-        for (int w = 0; w < min((int)(blockDim.x >> 5), 8); ++w) {
-            const int2 r = ranks[w];
-            if (w < at.warp) { back_rank += r.x; grow_rank += r.y; }
-            runs_back += r.x; runs_grow += r.y;
+        if (at.slot == 0) {
+            a.n_free_out[row] = n_free - sum.y_all;
+            if (a.short_out) a.short_out[row] = 0;
         }
+        return;
     }
+    Run *back_run = runs[ONE ? at.warp : 0][0], *grow_run = runs[ONE ? at.warp : 0][1];
+    back_rank += ONE ? 0 : sum.w & 1023; grow_rank += ONE ? 0 : sum.w >> 10 & 1023;
     int A = 0;
-    long long lacking = 0;
+    long long want = 0;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         if (at.slot + i >= c.B) break;
@@ -415,35 +405,39 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
         if (less > 0) back_run[back_rank++] = {sum.x + less, (at.slot + i) * c.T + need[i] - sum.x};
         sum.x += less;
         // a sum over all demands up to this one: the first that does not fit keeps out the ones behind it
-        const int upto = sum.y + (need[i] <= c.T ? more : 0);
-        const bool fits = need[i] <= c.T && upto <= n_free + R;
-        if (more > 0 && need[i] <= c.T) grow_run[grow_rank++] = {fits ? upto : sum.y, (at.slot + i) * c.T + have[i] - sum.y};
+        const bool fits_row = need[i] <= c.T;
+        const int upto = sum.y + (fits_row ? more : 0);
+        const bool served = fits_row && upto <= n_free + R;
+        if (more > 0 && fits_row) grow_run[grow_rank++] = {served ? upto : sum.y, (at.slot + i) * c.T + have[i] - sum.y};
         sum.y = upto;
-        if (fits) A = upto; else lacking += more;
-        a.n_blocks_out[slots + at.slot + i] = have[i] + (fits ? more : 0) - less;
+        if (served) A = upto;
+        want += more;
+        a.n_blocks_out[slots + at.slot + i] = have[i] + (served ? more : 0) - less;
     }
-    A = (int)__reduce_max_sync(kFull, (unsigned)A);
-    if (__any_sync(kFull, lacking != 0))
-        for (int o = 16; o > 0; o >>= 1) lacking += __shfl_xor_sync(kFull, lacking, o);
-    if (!ONE && at.lane == 0 && at.warp < 8) { granted[at.warp] = A; lacks[at.warp] = lacking; }
-    team_sync<ONE>();
-    if (!ONE) {
-        lacking = 0;
-        for (int w = 0; w < min((int)(blockDim.x >> 5), 8); ++w) { A = max(A, granted[w]); lacking += lacks[w]; }
+    if (all_fit) {
+        A = sum.y_all; want = A;
+        team_sync<ONE>();
+    } else {
+        A = (int)__reduce_max_sync(kFull, (unsigned)A);
+        for (int o = 16; o > 0; o >>= 1) want += __shfl_xor_sync(kFull, want, o);
+        if (!ONE && at.lane == 0) { granted[at.warp] = A; wanted[at.warp] = want; }
+        team_sync<ONE>();
+        if (!ONE) {
+            want = 0;
+            for (int w = 0; w < (int)(blockDim.x >> 5); ++w) { A = max(A, granted[w]); want += wanted[w]; }
+        }
     }
     if (at.slot == 0) {
         a.n_free_out[row] = n_free + R - A;
-        if (a.short_out) a.short_out[row] = (int)min(lacking, 0x7FFFFFFFll);
+        if (a.short_out) a.short_out[row] = (int)min(want - A, 0x7FFFFFFFll);
     }
     int lo, hi;
     cache_piece(at.piece, at.pieces, max(R, A), 0, &lo, &hi);
-    const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
-    const auto list = mk_span(c.free_list + row * c.P, c.P);
     const int both = min(R, A), top = n_free + R - 1;
-    move_items<true, true>(back_run, runs_back, grow_run, runs_grow, lo, min(hi, both), at.lane, table, list, top);
+    move_items<true, true>(back_run, n_back, grow_run, n_grow, lo, min(hi, both), at.lane, table, list, top);
     lo = max(lo, both);
-    if (R < A) move_items<false, true>(back_run, 0, grow_run, runs_grow, lo, hi, at.lane, table, list, top);
-    else move_items<true, false>(back_run, runs_back, grow_run, 0, lo, hi, at.lane, table, list, top);
+    if (R < A) move_items<false, true>(back_run, 0, grow_run, n_grow, lo, hi, at.lane, table, list, top);
+    else move_items<true, false>(back_run, n_back, grow_run, 0, lo, hi, at.lane, table, list, top);
 }
 
 // An entry with no other one of interest near it: 64 bytes of memory are fetched for it, not the usual 128.
@@ -486,7 +480,7 @@ __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
             ++count;
         }
     }
-    const TeamSums sum = team_sums<ONE>(count, 0, 0, part, at.lane, at.warp);
+    const TeamSums sum = team_sums<ONE, false>(count, 0, 0, 0, part, at.lane, at.warp);
     int place = sum.x;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
@@ -539,7 +533,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
         q[i] = min(max(q[i], 0), n[i]);
         mine = add_to_most(mine, q[i]);
     }
-    const TeamSums sum = team_sums<ONE>(mine, 0, 0, part, at.lane, at.warp);
+    const TeamSums sum = team_sums<ONE, true>(mine, 0, 0, 0, part, at.lane, at.warp);
     const auto cu = mk_span(a.cu + row * (c.B + 1), c.B + 1);
     const bool first_block = at.first_block();
     int place = sum.x;
@@ -625,7 +619,7 @@ __global__ void __launch_bounds__(256, 6) br_page_lists_kernel(const PageArgs a)
         mine += pages;
         counts += (n[i] > 0) + ((pages > 0) << 16);
     }
-    const TeamSums sum = team_sums<ONE>(mine, counts, 0, part, at.lane, at.warp);
+    const TeamSums sum = team_sums<ONE, false>(mine, counts, 0, 0, part, at.lane, at.warp);
     const auto seq_slot = mk_span(a.seq_slot + slots, c.B), last = mk_span(a.last + slots, c.B);
     const auto indptr = mk_span(a.indptr + row * (c.B + 1), c.B + 1);
     const bool first_block = at.first_block();
