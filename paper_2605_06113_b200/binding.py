@@ -363,7 +363,7 @@ class BlockCache:
 
     def __init__(self, table, n_blocks, free_list, n_free, block_tokens):
         import torch
-        self.torch, self._int32 = torch, torch.int32
+        self.torch, self._int32, self._int64 = torch, torch.int32, torch.int64
         if table.dim() != 4 or free_list.dim() != 3:
             raise ValueError("BlockCache: table is [N, G, B, columns] and free_list [N, G, pool]")
         self.device = table.device
@@ -371,12 +371,15 @@ class BlockCache:
         self.pool, self.block_tokens = free_list.shape[2], int(block_tokens)
         self._fleet, self._worker, self._slot = (self.N,), (self.N, self.G), (self.N, self.G, self.B)
         self._cu = (self.N, self.G, self.B + 1)
-        self._check((table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
-                    (free_list, "free_list", (*self._worker, self.pool)), (n_free, "n_free", self._worker))
+        self._list = (*self._worker, self.pool)
+        self._refuse((table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
+                     (free_list, "free_list", self._list), (n_free, "n_free", self._worker))
         self.table, self.n_blocks, self.free_list, self.n_free = table, n_blocks, free_list, n_free
         self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, table.data_ptr(),
                                    n_blocks.data_ptr(), free_list.data_ptr(), n_free.data_ptr())
+        self._index = table.get_device()                     # -1: not on a GPU
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
     @classmethod
     def empty(cls, N, G, B, block_tokens, pool_blocks, table_blocks, device="cuda:0"):
@@ -387,9 +390,12 @@ class BlockCache:
         return cls(torch.zeros((N, G, B, table_blocks), **z), torch.zeros((N, G, B), **z), free,
                    torch.full((N, G), pool_blocks, **z), block_tokens)
 
-    def _check(self, *arrays):
+    def _is(self, t, shape):
+        return t.dtype is self._int32 and t.shape == shape and t.get_device() == self._index and t.is_contiguous()
+
+    def _refuse(self, *arrays):
         for t, name, shape in arrays:
-            if t.dtype is not self._int32 or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            if t is not None and (t.dtype is not self._int32 or t.shape != shape or t.device != self.device or not t.is_contiguous()):
                 raise ValueError(f"{name}: needs a contiguous int32 tensor {list(shape)} on {self.device}, "
                                  f"got {t.dtype} {list(t.shape)} on {t.device}")
 
@@ -399,10 +405,10 @@ class BlockCache:
         if first < 0 or N < 0 or first + N > self.N:
             raise ValueError(f"rows {first} to {first + N}: the cache has {self.N}")
         if stream is None:
-            if self.device.type != "cuda":
+            if self._index < 0:
                 stream = 0
             elif self._raw_stream is not None:
-                stream = self._raw_stream(self.device.index)
+                stream = self._raw_stream(self._index)
             else:
                 stream = self.torch.cuda.current_stream(self.device).cuda_stream
         elif isinstance(stream, C.c_void_p):
@@ -415,7 +421,7 @@ class BlockCache:
         if self.N == 0:
             return                                           # (empty tensors have no address)
         fn = getattr(lib(), name)
-        if self.device.type == "cuda" and self.torch.cuda.current_device() != self.device.index:
+        if self._index >= 0 and self._current_device() != self._index:
             with self.torch.cuda.device(self.device):       # the launch goes to the tensors' device
                 rc = fn(*args)
         else:
@@ -429,38 +435,42 @@ class BlockCache:
         (default: the cache's own, in place)."""
         nb = self.n_blocks if n_blocks_out is None else n_blocks_out
         nf = self.n_free if n_free_out is None else n_free_out
-        self._check((length, "length", self._slot), (nb, "n_blocks_out", self._slot), (nf, "n_free_out", self._worker))
-        if step is not None:
-            self._check((step, "step", self._fleet))
-        if short_blocks is not None:
-            self._check((short_blocks, "short_blocks", self._worker))
-        self._call("br_block_tables", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step),
-                   nb.data_ptr(), nf.data_ptr(), _ptr(short_blocks))
+        ok, slot, worker = self._is, self._slot, self._worker
+        if not (ok(length, slot) and ok(nb, slot) and ok(nf, worker) and (step is None or ok(step, self._fleet)) and
+                (short_blocks is None or ok(short_blocks, worker))):
+            self._refuse((length, "length", slot), (nb, "n_blocks_out", slot), (nf, "n_free_out", worker),
+                         (step, "step", self._fleet), (short_blocks, "short_blocks", worker))
+        self._call("br_block_tables", self._batch(N, first, stream), self._packed, length.data_ptr(),
+                   None if step is None else step.data_ptr(), nb.data_ptr(), nf.data_ptr(),
+                   None if short_blocks is None else short_blocks.data_ptr())
 
     def slot_map(self, length, cu, slots, n_new=None, step=None, N=None, first=0, stream=None):
         """Cache slots of the newest ``n_new`` tokens of each request (default: one of each running request) into ``slots``
         [N, G, room] int64, with prefix sums ``cu`` [N, G, B + 1]."""
-        self._check((length, "length", self._slot), (cu, "cu", self._cu))
-        if n_new is not None:
-            self._check((n_new, "n_new", self._slot))
-        if step is not None:
-            self._check((step, "step", self._fleet))
-        if slots.dtype is not self.torch.int64 or slots.dim() != 3 or slots.shape[:2] != self._worker or \
-                slots.device != self.device or not slots.is_contiguous():
+        ok, slot = self._is, self._slot
+        if not (ok(length, slot) and ok(cu, self._cu) and (n_new is None or ok(n_new, slot)) and
+                (step is None or ok(step, self._fleet))):
+            self._refuse((length, "length", slot), (cu, "cu", self._cu), (n_new, "n_new", slot), (step, "step", self._fleet))
+        room = slots.shape[-1] if slots.dim() == 3 else -1
+        if slots.dtype is not self._int64 or slots.shape != (*self._worker, room) or slots.get_device() != self._index or \
+                not slots.is_contiguous():
             raise ValueError(f"slots: needs a contiguous int64 tensor [{self.N}, {self.G}, room] on {self.device}, "
                              f"got {slots.dtype} {list(slots.shape)} on {slots.device}")
-        self._call("br_slot_map", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step), _ptr(n_new),
-                   slots.shape[2], cu.data_ptr(), slots.data_ptr())
+        self._call("br_slot_map", self._batch(N, first, stream), self._packed, length.data_ptr(),
+                   None if step is None else step.data_ptr(), None if n_new is None else n_new.data_ptr(), room,
+                   cu.data_ptr(), slots.data_ptr())
 
     def page_lists(self, length, n_seq, seq_slot, indptr, indices, last_tokens, step=None, N=None, first=0, stream=None):
         """The running requests packed, with their blocks one after another."""
-        self._check((length, "length", self._slot), (n_seq, "n_seq", self._worker), (seq_slot, "seq_slot", self._slot),
-                    (indptr, "indptr", self._cu), (indices, "indices", (self.N, self.G, self.pool)),
-                    (last_tokens, "last_tokens", self._slot))
-        if step is not None:
-            self._check((step, "step", self._fleet))
-        self._call("br_page_lists", self._batch(N, first, stream), self._packed, length.data_ptr(), _ptr(step),
-                   n_seq.data_ptr(), seq_slot.data_ptr(), indptr.data_ptr(), indices.data_ptr(), last_tokens.data_ptr())
+        ok, slot = self._is, self._slot
+        if not (ok(length, slot) and ok(n_seq, self._worker) and ok(seq_slot, slot) and ok(indptr, self._cu) and
+                ok(indices, self._list) and ok(last_tokens, slot) and (step is None or ok(step, self._fleet))):
+            self._refuse((length, "length", slot), (n_seq, "n_seq", self._worker), (seq_slot, "seq_slot", slot),
+                         (indptr, "indptr", self._cu), (indices, "indices", self._list), (last_tokens, "last_tokens", slot),
+                         (step, "step", self._fleet))
+        self._call("br_page_lists", self._batch(N, first, stream), self._packed, length.data_ptr(),
+                   None if step is None else step.data_ptr(), n_seq.data_ptr(), seq_slot.data_ptr(), indptr.data_ptr(),
+                   indices.data_ptr(), last_tokens.data_ptr())
 
 
 def state_to_numpy(st) -> Dict[str, np.ndarray]:

@@ -237,10 +237,12 @@ struct Windows {
         for (int u = 0; u < kMoves; ++u) shift[u] = only;
         if (in == 0) return true;
         int count = __popc(in);
-        if (count == 1) {
-            const int from = __shfl_sync(kFull, d, 0) - lane, then = runs[++run].shift;
+        if (count <= 3) {                   // (counting bits costs as much as four runs one by one)
+            for (int k = 0; k < count; ++k) {
+                const int from = __shfl_sync(kFull, d, k) - lane, then = runs[++run].shift;
 #pragma unroll
-            for (int u = 0; u < kMoves; ++u) shift[u] = 32 * u >= from ? then : only;
+                for (int u = 0; u < kMoves; ++u) shift[u] = 32 * u >= from ? then : shift[u];
+            }
             return false;
         }
         unsigned starts[kMoves];
@@ -266,6 +268,14 @@ struct Windows {
     }
 };
 
+// An entry with no other one of interest near it: 64 bytes of memory are fetched for it, not the usual 128.
+__device__ __forceinline__ int lone_entry(const int32_t *p)
+{
+    int v;
+    asm volatile("ld.global.L2::64B.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // Moves items [lo, hi) of a warp, kMoves of a lane at a time: item x is entry x + shift of its run in `table`, or entry top - x
 // of `list`.
 template <bool FROM_TABLE, bool TO_TABLE, typename Table, typename List>
@@ -288,7 +298,7 @@ __device__ __forceinline__ void move_items(const Run *from_runs, int n_from, con
         } else {
 #pragma unroll
             for (int u = 0; u < kMoves; ++u)
-                if (e + 32 * u < hi) id[u] = FROM_TABLE ? table[e + 32 * u + shift[u]] : list[top - e - 32 * u];
+                if (e + 32 * u < hi) id[u] = FROM_TABLE ? lone_entry(&table[e + 32 * u + shift[u]]) : list[top - e - 32 * u];
         }
         const bool one_to = TO_TABLE ? to.next(e0, lane, shift) : true;
         if (full && one_to) {
@@ -331,37 +341,40 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
     const size_t row = at.row, slots = row * c.B;
     const int step = at.step(c), n_free = c.n_free[row];
     int need[SPL], have[SPL], held = 0, back = 0, ask = 0;
-    bool bad = false, too_long = false, several = false;
+    int flags = 0;                          // some slot's count is out of range, its request is too long, it grows by several blocks
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         need[i] = BR_EMPTY_SLOT; have[i] = 0;
         if (at.slot + i < c.B) { need[i] = c.len[slots + at.slot + i]; have[i] = c.n_blocks[slots + at.slot + i]; }
     }
-    // the slots that give blocks back, and those that ask for some, are counted: their runs are packed
-    int back_rank = 0, grow_rank = 0, n_back = 0, n_grow = 0;
-    const unsigned below = (1u << at.lane) - 1;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         need[i] = cache_blocks(c, cache_tokens(need[i], step));
         const bool in_range = (unsigned)have[i] <= (unsigned)c.T, fits_row = need[i] <= c.T;
         const int more = in_range ? need[i] - have[i] : 0;
-        bad = bad || !in_range;
-        too_long = too_long || !fits_row;
-        several = several || more > 1;
+        flags |= (in_range ? 0 : 1 << 20) | (fits_row ? 0 : 1 << 24) | (more > 1 ? 1 << 28 : 0);
         held += in_range ? have[i] : 0;
         back += max(-more, 0);
         ask += fits_row ? max(more, 0) : 0;
-        const unsigned backs = __ballot_sync(kFull, more < 0), grows = __ballot_sync(kFull, more > 0 && fits_row);
-        back_rank += __popc(backs & below); grow_rank += __popc(grows & below);
-        n_back += __popc(backs); n_grow += __popc(grows);
     }
-    const int flags = (__any_sync(kFull, bad) ? 1 << 20 : 0) + (__any_sync(kFull, too_long) ? 1 << 24 : 0) +
-                      (__any_sync(kFull, several) ? 1 << 28 : 0);
+    flags = (int)__reduce_or_sync(kFull, (unsigned)flags);
+    // the slots that give blocks back, and those that ask for some, are counted: their runs are packed
+    int back_rank = 0, grow_rank = 0, n_back = 0, n_grow = 0;
+    const auto rank = [&] {
+        const unsigned below = (1u << at.lane) - 1;
+#pragma unroll
+        for (int i = 0; i < SPL; ++i) {
+            const unsigned backs = __ballot_sync(kFull, have[i] > need[i]), grows = __ballot_sync(kFull, need[i] > have[i] && need[i] <= c.T);
+            back_rank += __popc(backs & below); grow_rank += __popc(grows & below);
+            n_back += __popc(backs); n_grow += __popc(grows);
+        }
+    };
+    if (!ONE) rank();
     // (with counts in range all sums stay below 2^30; counts and flags take ten and four bits, from eight warps)
     TeamSums sum = team_sums<ONE, false>(back, ask, held, n_back + (n_grow << 10) + flags, part, at.lane, at.warp);
-    n_back = sum.w_all & 1023; n_grow = sum.w_all >> 10 & 1023;
-    bad = (sum.w_all & 15 << 20) != 0 || (unsigned)n_free > (unsigned)c.P || n_free + sum.z_all > c.P;
-    too_long = (sum.w_all & 15 << 24) != 0; several = ((unsigned)sum.w_all >> 28) != 0;
+    if (!ONE) { n_back = sum.w_all & 1023; n_grow = sum.w_all >> 10 & 1023; }
+    const bool bad = (sum.w_all & 15 << 20) != 0 || (unsigned)n_free > (unsigned)c.P || n_free + sum.z_all > c.P;
+    const bool too_long = (sum.w_all & 15 << 24) != 0, several = ((unsigned)sum.w_all >> 28) != 0;
     if (bad) {                              // counts that no sequence of updates leaves behind: the worker stays as it is
 #pragma unroll
         for (int i = 0; i < SPL; ++i)
@@ -395,7 +408,7 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
         return;
     }
     Run *back_run = runs[ONE ? at.warp : 0][0], *grow_run = runs[ONE ? at.warp : 0][1];
-    back_rank += ONE ? 0 : sum.w & 1023; grow_rank += ONE ? 0 : sum.w >> 10 & 1023;
+    if (ONE) rank(); else { back_rank += sum.w & 1023; grow_rank += sum.w >> 10 & 1023; }
     int A = 0;
     long long want = 0;
 #pragma unroll
@@ -438,14 +451,6 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
     lo = max(lo, both);
     if (R < A) move_items<false, true>(back_run, 0, grow_run, n_grow, lo, hi, at.lane, table, list, top);
     else move_items<true, false>(back_run, n_back, grow_run, 0, lo, hi, at.lane, table, list, top);
-}
-
-// An entry with no other one of interest near it: 64 bytes of memory are fetched for it, not the usual 128.
-__device__ __forceinline__ int lone_entry(const int32_t *p)
-{
-    int v;
-    asm volatile("ld.global.L2::64B.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
 }
 
 // One new token a request.
