@@ -248,6 +248,10 @@ class Router:
             return stream.value
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
+    def block_cache(self, N: int, block_tokens: int, pool_blocks: int, table_blocks: int) -> "BlockCache":
+        """A new paged cache for the workers of N fleets of this shape."""
+        return BlockCache.empty(N, self.cfg.G, self.cfg.B, block_tokens, pool_blocks, table_blocks, device=self.device)
+
     # ---- the calls of include/br.h -------------------------------------------
     def step(self, st, out, term_probs=None, N=None, first=0, n_steps=1, stream=None):
         if N is None:
@@ -374,12 +378,25 @@ class BlockCache:
         self._list = (*self._worker, self.pool)
         self._refuse((table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
                      (free_list, "free_list", self._list), (n_free, "n_free", self._worker))
-        self.table, self.n_blocks, self.free_list, self.n_free = table, n_blocks, free_list, n_free
-        self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, table.data_ptr(),
-                                   n_blocks.data_ptr(), free_list.data_ptr(), n_free.data_ptr())
+        self._table, self._free_list = table, free_list
+        self._keep(n_blocks, n_free)
         self._index = table.get_device()                     # -1: not on a GPU
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+    # (read-only: the calls use the tensors that the handle was made with, or the counts of the last commit)
+    table, free_list = property(lambda self: self._table), property(lambda self: self._free_list)
+    n_blocks, n_free = property(lambda self: self._n_blocks), property(lambda self: self._n_free)
+
+    def _keep(self, n_blocks, n_free):
+        self._n_blocks, self._n_free = n_blocks, n_free
+        self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, self._table.data_ptr(),
+                                   n_blocks.data_ptr(), self._free_list.data_ptr(), n_free.data_ptr())
+
+    def commit(self, n_blocks, n_free):
+        """Takes the counts that an update wrote to other tensors as the cache's own (the old tensors are free again)."""
+        self._refuse((n_blocks, "n_blocks", self._slot), (n_free, "n_free", self._worker))
+        self._keep(n_blocks, n_free)
 
     @classmethod
     def empty(cls, N, G, B, block_tokens, pool_blocks, table_blocks, device="cuda:0"):
@@ -432,7 +449,7 @@ class BlockCache:
     def block_tables(self, length, n_blocks_out=None, n_free_out=None, short_blocks=None, step=None, N=None, first=0,
                      stream=None):
         """Brings tables and free lists in line with the lengths; the new counts go to ``n_blocks_out`` and ``n_free_out``
-        (default: the cache's own, in place)."""
+        (default: the cache's own, in place).  With other tensors the cache stays as it was until ``commit`` takes them."""
         nb = self.n_blocks if n_blocks_out is None else n_blocks_out
         nf = self.n_free if n_free_out is None else n_free_out
         ok, slot, worker = self._is, self._slot, self._worker

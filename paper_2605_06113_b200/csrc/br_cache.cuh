@@ -313,13 +313,13 @@ __device__ __forceinline__ void move_items(const Run *from_runs, int n_from, con
     }
 }
 
-// Items [lo, hi) of `count` for one of `pieces`: equal numbers of units of 128, counted from `skew` items ahead of the first.
-__device__ __forceinline__ void cache_piece(int piece, int pieces, int count, int skew, int *lo, int *hi)
+// Items [lo, hi) of `count` for one of `pieces`: equal numbers of units, counted from `skew` items ahead of the first.
+__device__ __forceinline__ void cache_piece(int piece, int pieces, int count, int skew, int unit, int *lo, int *hi)
 {
     if (pieces == 1) { *lo = 0; *hi = count; return; }
-    const int units = (count + skew + 127) / 128, each = (units + pieces - 1) / pieces;
-    *lo = max(0, (int)min((long long)count, (long long)each * piece * 128 - skew));
-    *hi = (int)min((long long)count, (long long)each * (piece + 1) * 128 - skew);
+    const int units = (count + skew + unit - 1) / unit, each = (units + pieces - 1) / pieces;
+    *lo = max(0, (int)min((long long)count, (long long)each * piece * unit - skew));
+    *hi = (int)min((long long)count, (long long)each * (piece + 1) * unit - skew);
 }
 
 // Block a of the growth (in slot and table order) is block a of those taken back (same order) while there are any, then the
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
         if (a.short_out) a.short_out[row] = (int)min(want - A, 0x7FFFFFFFll);
     }
     int lo, hi;
-    cache_piece(at.piece, at.pieces, max(R, A), 0, &lo, &hi);
+    cache_piece(at.piece, at.pieces, max(R, A), 0, 32 * kMoves, &lo, &hi);
     const int both = min(R, A), top = n_free + R - 1;
     move_items<true, true>(back_run, n_back, grow_run, n_grow, lo, min(hi, both), at.lane, table, list, top);
     lo = max(lo, both);
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     // items are counted from the 32-byte boundary at or ahead of the row's first one (room is at most 2^30)
     const int skew = (int)(reinterpret_cast<uintptr_t>(a.slots + row * a.room) >> 3) & 3;
     int lo, hi;
-    cache_piece(at.piece, at.pieces, count, skew, &lo, &hi);
+    cache_piece(at.piece, at.pieces, count, skew, 128, &lo, &hi);
     int e = (lo + skew) / 128 * 128 - skew + 4 * at.lane;     // (lo is at a unit's start, or the row's)
     if (max(e, lo) >= hi) return;
     Walk<TokenRun> w;
@@ -650,7 +650,7 @@ __global__ void __launch_bounds__(256, 6) br_page_lists_kernel(const PageArgs a)
     const auto table = mk_span(c.table + slots * c.T, (long long)c.B * c.T);
     const auto out = mk_span(a.indices + row * c.P, c.P);
     int lo, hi;
-    cache_piece(at.piece, at.pieces, min(sum.x_all, c.P), 0, &lo, &hi);
+    cache_piece(at.piece, at.pieces, min(sum.x_all, c.P), 0, 32 * kMoves, &lo, &hi);
     // (indices are a list that runs upwards: entry x of it is item x)
     move_items<true, false>(run, runs_all, run, 0, lo, hi, at.lane, table, UpList<decltype(out)>{out}, 0);
 }

@@ -114,6 +114,21 @@ def test_binding_refuses_tensors_of_another_type_shape_layout_or_device():
     BlockCache.empty(0, G, B, 16, P, T, device="cpu").block_tables(torch.zeros((0, G, B), **z))
 
 
+def test_counts_are_taken_by_commit_and_not_by_assignment():
+    c = BlockCache.empty(2, 3, 4, 16, 5, 6, device="cpu")
+    nb, nf = torch.ones_like(c.n_blocks), torch.ones_like(c.n_free)
+    for name in ("table", "n_blocks", "free_list", "n_free"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, nb)
+    before = c._packed
+    for bad in ((nb.long(), nf), (nb, nf[:1]), (nf, nb)):
+        with pytest.raises(ValueError):
+            c.commit(*bad)
+    assert c._packed == before
+    c.commit(nb, nf)
+    assert c.n_blocks is nb and c.n_free is nf and c._packed != before
+
+
 def test_new_cache_gives_out_blocks_from_zero():
     c = BlockCache.empty(2, 3, 4, 16, 5, 6, device="cpu")
     assert c.free_list.tolist() == [[[4, 3, 2, 1, 0]] * 3] * 2 and c.n_free.tolist() == [[5] * 3] * 2

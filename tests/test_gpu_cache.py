@@ -16,7 +16,9 @@ DEV = "cuda:0"
 # N, G, B, tokens a block, blocks a pool, columns a row
 SHAPES = [(1, 1, 1, 1, 1, 1), (1, 4, 64, 16, 700, 90), (3, 5, 7, 24, 60, 31), (2, 3, 256, 16, 5000, 65), (70, 33, 8, 5, 97, 40),
           (300, 9, 33, 64, 150, 17), (1, 64, 40, 1, 900, 333), (2, 1, 65, 128, 4099, 1030), (1, 2, 9, 100, 3000, 2500),
-          (2500, 8, 16, 16, 64, 9), (5, 1, 255, 7, 33, 6), (1, 1, 130, 3, 20011, 1000)]
+          (5, 1, 255, 7, 33, 6), (1, 1, 130, 3, 20011, 1000)]
+# enough workers for teams of one warp, with one and two slots a lane, and for the smallest teams of wide workers
+BATCHES = [(2500, 8, 16, 16, 64, 9), (620, 8, 50, 16, 120, 11), (150, 8, 130, 16, 300, 12)]
 
 
 def _gpu(a):
@@ -77,14 +79,13 @@ def _walk(rng, f, n, ended, refill, grow):
     return np.where((n == 0) & (rng.random(n.shape) < refill), rng.integers(0, most + 1, n.shape), n)
 
 
-@pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("stepped", [False, True])
+@pytest.mark.parametrize("shape,stepped", [(s, k) for s in SHAPES for k in (False, True)] + [(s, True) for s in BATCHES])
 def test_walks_of_lengths(shape, stepped):
     p = Pair(*shape, seed=sum(shape))
     f = p.f
     rng = np.random.default_rng(17 * sum(shape) + stepped)
     n = np.zeros((f.N, f.G, f.B), np.int64)
-    big = f.N * f.G > 500
+    big = f.N * f.G > 1000
     for k, (ended, refill, grow) in enumerate([(0, 0.7, 1), (0.0, 0.0, 1), (0.3, 0.6, 5), (0.01, 0.1, 1), (0.9, 0.2, 40)][:3 if big else 5]):
         n = _walk(rng, f, n, ended, refill, grow)
         step = rng.integers(-5, 10 ** 6, f.N).astype(np.int32) if stepped else None
@@ -141,6 +142,23 @@ def test_undoing_an_update_restores_tables_and_lists():
     listed = torch.arange(900, device=DEV) < nf[..., None]
     assert torch.equal(torch.where(held, table, 0), torch.where(held, p.c.table, 0))
     assert torch.equal(torch.where(listed, free, 0), torch.where(listed, p.c.free_list, 0))
+
+
+@pytest.mark.parametrize("N,G", [(3, 8), (300, 8)])
+def test_updates_in_turns_between_two_sets_of_counts(N, G):
+    p = Pair(N, G, 50, 16, 700, 40, seed=6)
+    rng = np.random.default_rng(7)
+    n = np.zeros((N, G, 50), np.int64)
+    spare = (torch.empty_like(p.c.n_blocks), torch.empty_like(p.c.n_free))
+    for _ in range(6):
+        n = _walk(rng, p.f, n, 0.2, 0.6, 3)
+        p.c.block_tables(_gpu(n.astype(np.int32)), *spare)
+        spare, old = (p.c.n_blocks, p.c.n_free), spare
+        p.c.commit(*old)
+        p.f.update(n.astype(np.int32))
+        p.same()
+        p.pages(n.astype(np.int32))
+    p.f.check_partition()
 
 
 @pytest.mark.parametrize("workers", [(1, 3), (900, 7)])
@@ -333,6 +351,9 @@ def test_beside_the_routing_step(name, kw, n_inst, steps):
     r = Router(wl, device=DEV)
     st, out = r.device_state(), r.outputs(n_inst)
     p = Pair(n_inst, cfg.G, cfg.B, 16, 2600, 2100, seed=41)
+    p.c = r.block_cache(n_inst, 16, 2600, 2100)
+    p.f.free_list[:] = np.arange(2599, -1, -1)
+    p.c.table.fill_(-9)
     z = dict(dtype=torch.int32, device=DEV)
     f = p.f
     cu, slots = torch.zeros((n_inst, f.G, f.B + 1), **z), torch.zeros((n_inst, f.G, f.B), dtype=torch.int64, device=DEV)
@@ -365,3 +386,33 @@ def test_beside_the_routing_step(name, kw, n_inst, steps):
     r.fscore(s, load, F, cap=p.c.n_free, best_g=best)
     assert not bool((best == 1).any())
     r.close()
+
+
+def test_range_checked_build():
+    """libbr_dbg.so counts indexes outside a row of the tables, lists and outputs: there are none, on teams of every size, with
+    runs long and short, counts that cannot be, and rows of outputs that are too small."""
+    from paper_2605_06113_b200 import binding, build
+    binding.use_library(build.build_debug())
+    try:
+        hits = binding.lib().br_debug_bounds_hits()
+        assert hits >= 0
+        rng = np.random.default_rng(9)
+        for shape in ((1, 1, 1, 1, 1, 1), (1, 4, 64, 16, 700, 90), (2, 3, 256, 16, 5000, 65), (1300, 8, 33, 5, 97, 40), (5, 1, 130, 7, 33, 6)):
+            p = Pair(*shape, seed=13)
+            n = np.zeros(p.f.n_blocks.shape, np.int64)
+            for k in range(3):
+                n = _walk(rng, p.f, n, 0.3, 0.7, 4)
+                length = n.astype(np.int32)
+                p.update(length, out=k == 1)
+                p.slots(length, p.f.B)
+                p.slots(length, 1 + 5 * k * p.f.B, rng.integers(0, 50, n.shape).astype(np.int32))
+                p.pages(length)
+            for value in (MOST, -5):
+                p.f.n_blocks[0, 0, 0] = value
+                p.c.n_blocks[0, 0, 0] = value
+                p.update(length)
+                p.slots(length, 9, np.full(n.shape, 3, np.int32))
+                p.pages(length)
+        assert binding.lib().br_debug_bounds_hits() == hits
+    finally:
+        binding.use_library(None)
