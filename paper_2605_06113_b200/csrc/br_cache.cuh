@@ -12,6 +12,11 @@
 // A team of warps takes one worker: a single warp where there are workers enough to fill the GPU (eight of them a block), a
 // block otherwise.  Each thread owns one or two slots, and one exchange of the warps' sums gives every slot its place.  What
 // is to be moved is then cut into equal pieces by items, not by slots, so one long request is spread like many short ones.
+//
+// Large calls are bound by memory: 16 of the largest fleets' page lists (37.8 million blocks) take 53.9 us, 0.81 of the
+// measured copy bandwidth, 146 million prompt tokens 200 us, 0.90.  Calls between two decode steps move next to nothing and
+// are bound by the launch and two trips to memory: 2.0 us for four workers, 6.5 us for 8,192, a tenth of which take a prompt.
+// (Device times of captured calls.)
 #pragma once
 #include <algorithm>
 #include "br_device.cuh"
@@ -64,24 +69,31 @@ struct PageArgs {
     int32_t *n_seq, *seq_slot, *indptr, *indices, *last;
 };
 
-// The team of a worker, and how many slots a thread of it owns (one or two).
+// The team of a worker, how many slots a thread of it owns (one or two), and how many blocks share the worker.
 struct CacheShape { int warps, spl, slices; };
 
-// pieces: the pieces that what a worker moves may be cut into at most; limit: warps a block at most
-inline CacheShape cache_shape(int B, int workers, int pieces, int limit)
+// Warps a worker for calls that move up to `items` items of it, at most `limit`: more while all of them are on the GPU at once
+// and each has more than 256 items, or up to four rounds of them while each has 2,048 or more, which evens out workers that
+// move different amounts.  (Page lists of 8,192 workers of 130 requests' blocks each: 112 us with one warp a worker, 98 with
+// four; chunks of their prompts 238, 179; page lists of 2,107 workers of up to 9,999 blocks 25 us with four warps in one round,
+// 33 in two.)
+inline CacheShape cache_shape(int B, int workers, long long items, int limit)
 {
     CacheShape s = {1, 1, 1};
     while (s.warps * 64 < B) s.warps *= 2;
-    while (s.warps < limit && s.warps < pieces && 2ll * s.warps * workers <= kCacheWarps) s.warps *= 2;
+    const auto worth = [&](long long warps) {
+        return (warps * workers <= kCacheWarps && items > 256 * warps) || (warps * workers <= 4 * kCacheWarps && items >= 2048 * warps);
+    };
+    while (s.warps < limit && worth(2 * s.warps)) s.warps *= 2;
     s.spl = 32 * s.warps >= B ? 1 : 2;
     return s;
 }
 
-// A team for copies of up to `items` items a worker.  Several blocks a worker where that fills the GPU with warps of 512 items
-// or more, or evens out the workers' different loads over four rounds of warps of 2,048 or more.
+// ... and blocks a worker, by the same rule with pieces of 512 and of 2,048 items a warp, for calls that only copy: 146 million
+// prompt tokens of 256 workers 605 us with one block of eight warps each, 216 with 8, 200 with 18.
 inline CacheShape cache_copy_shape(int B, int workers, int items)
 {
-    CacheShape s = cache_shape(B, workers, (items + 511) / 512, 8);
+    CacheShape s = cache_shape(B, workers, items, 8);
     if (s.warps > 1) {
         const long long warps = (long long)workers * s.warps;
         const long long fill = std::min(kCacheWarps / warps, (long long)items / (512 * s.warps));
@@ -217,8 +229,11 @@ template <typename Out> struct UpList {
     __device__ __forceinline__ auto &operator[](int i) const { return out[-i]; }
 };
 
-// The runs of the items of one warp, window by window of kMoves rows of 32: a bit for each item that starts a run turns into
-// the run of every item by counting bits, which has no loop that lanes leave one by one.  No run is empty.
+// The runs of the items of one warp, window by window of kMoves rows of 32.  Where one run covers a window, the rule for long
+// requests, its items are a constant apart; up to three starts are compared with every item; with more of them a bit for each
+// item that starts a run turns into the run of every item by counting bits, which has no loop that lanes leave one by one.  No
+// run is empty.  (Lanes that walk through the runs one by one: page lists of 2,107 workers with runs of 33 blocks 29.5 us, 25.1
+// this way; windows of 128 items: filling 1,024 caches 80.6 us, 62 with 256.)
 struct Windows {
     const Run *runs;
     int n, run;                             // run: that of the window's first item
@@ -268,7 +283,8 @@ struct Windows {
     }
 };
 
-// An entry with no other one of interest near it: 64 bytes of memory are fetched for it, not the usual 128.
+// An entry with few others of interest near it: 64 bytes of memory are fetched for it, not the usual 128 (newest tokens of
+// 32,768 workers' requests: 43.1 us with plain loads, 28.7 this way; 259 MB read from DRAM, 138).
 __device__ __forceinline__ int lone_entry(const int32_t *p)
 {
     int v;
@@ -390,7 +406,7 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
     const auto list = mk_span(c.free_list + row * c.P, c.P);
     const bool all_fit = !too_long && sum.y_all <= n_free + R;
     // between two decode steps most workers only grow, by a block a request at most, and all of it fits: each thread serves
-    // its own slots
+    // its own slots (four workers 3.05 us by the way below, 2.0 by this one)
     if (R == 0 && all_fit && !several) {
         int id[SPL];
 #pragma unroll
@@ -401,6 +417,7 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
             if (need[i] > have[i]) table[(at.slot + i) * c.T + have[i]] = id[i];
             a.n_blocks_out[slots + at.slot + i] = need[i];
         }
+        if (ONE) __syncwarp();              // (every lane has read n_free, which may be n_free_out)
         if (at.slot == 0) {
             a.n_free_out[row] = n_free - sum.y_all;
             if (a.short_out) a.short_out[row] = 0;
@@ -502,10 +519,15 @@ __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
 
 struct alignas(32) FourSlots { long long v[4]; };
 
-// 32 bytes in one store, so that every sector is written whole and once (two of 16 bytes wrote each sector twice)
+// 32 bytes in one store, so that every sector is written whole and once (two of 16 bytes wrote each sector twice, 296 us for 146
+// million tokens; 219 this way)
 __device__ __forceinline__ void store_four(FourSlots *p, const FourSlots &s)
 {
+#ifdef BR_BOUNDS
+    for (int j = 0; j < 4; ++j) p->v[j] = s.v[j];                  // (the sink of an index out of range is not that aligned)
+#else
     asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" :: "l"(p), "l"(s.v[0]), "l"(s.v[1]), "l"(s.v[2]), "l"(s.v[3]) : "memory");
+#endif
 }
 
 // Any number of new tokens: four in a row a lane, stored as 32 aligned bytes.
@@ -522,7 +544,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     TokenRun *run = runs[ONE ? at.warp : 0];
     const size_t row = at.row, slots = row * c.B;
     const int step = at.step(c);
-    int n[SPL], q[SPL], held[SPL], mine = 0;
+    int n[SPL], q[SPL], held[SPL], mine = 0, some = 0;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         n[i] = BR_EMPTY_SLOT; q[i] = held[i] = 0;
@@ -537,11 +559,12 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
         n[i] = cache_tokens(n[i], step);
         q[i] = min(max(q[i], 0), n[i]);
         mine = add_to_most(mine, q[i]);
+        some += q[i] > 0;
     }
-    const TeamSums sum = team_sums<ONE, true>(mine, 0, 0, 0, part, at.lane, at.warp);
+    const TeamSums sum = team_sums<ONE, true>(mine, some, 0, 0, part, at.lane, at.warp);
     const auto cu = mk_span(a.cu + row * (c.B + 1), c.B + 1);
     const bool first_block = at.first_block();
-    int place = sum.x;
+    int place = sum.x, rank = sum.y;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
         const int b = at.slot + i;
@@ -549,7 +572,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
         const int from = place;
         place = add_to_most(place, q[i]);
         // (a run that starts at 2^31 - 1 has no item below `room`)
-        run[b] = {place, n[i] - q[i] - from, b * c.T, min(max(held[i], 0), c.T)};
+        if (q[i] > 0) run[rank++] = {place, n[i] - q[i] - from, b * c.T, min(max(held[i], 0), c.T)};
         if (first_block) {
             cu[b] = from;
             if (b == c.B - 1) cu[c.B] = place;
@@ -566,7 +589,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     int e = (lo + skew) / 128 * 128 - skew + 4 * at.lane;     // (lo is at a unit's start, or the row's)
     if (max(e, lo) >= hi) return;
     Walk<TokenRun> w;
-    w.seek(run, c.B, max(e, lo));
+    w.seek(run, sum.y_all, max(e, lo));
     for (; e < hi; e += 128) {
         w.to(max(e, lo));
         const int p = e + w.at.shift, column = over(max(p, 0), c.over_t), offset = p - column * c.t;
@@ -587,7 +610,7 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
                 if (e + j < lo || e + j >= hi) continue;
                 w.to(e + j);
                 const int pj = e + j + w.at.shift, cj = over(pj, c.over_t);
-                if (cj < w.at.held) { off[j] = pj - cj * c.t; id[j] = table[w.at.base + cj]; }
+                if (cj < w.at.held) { off[j] = pj - cj * c.t; id[j] = lone_entry(&table[w.at.base + cj]); }
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)

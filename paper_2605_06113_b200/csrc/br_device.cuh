@@ -21,7 +21,7 @@ enum : uint32_t { kStreamArrCount = 0, kStreamArrLen = 1, kStreamTerm = 2, kStre
 // assert).  The host reads the count with br_debug_bounds_hits().  In the normal build span_t<T>
 // is a plain pointer and the helpers below vanish.
 #ifdef BR_BOUNDS
-__device__ __align__(32) unsigned long long g_bounds_sink[8];
+__device__ unsigned long long g_bounds_sink[8];
 __device__ unsigned g_bounds_hits;
 
 template <typename T>

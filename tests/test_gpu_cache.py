@@ -213,11 +213,13 @@ def test_cache_slots_beyond_32_bits():
     assert (p.f.table[p.f.table >= 0].astype(np.int64) * t).max() > 2 ** 32
 
 
-def test_tables_beyond_32_bits():
-    G, B, T = 64, 256, 140001                                     # 2.29e9 entries
+def test_arrays_beyond_32_bits():
+    """Tables, free lists, page lists and slot maps of more than 2^31 entries: the last workers' rows are behind that."""
+    G, B, T, P, room = 64, 256, 140001, 34000001, 34000001
     z = dict(dtype=torch.int32, device=DEV)
-    c = BlockCache(torch.empty((1, G, B, T), **z), torch.zeros((1, G, B), **z),
-                   torch.arange(999, -1, -1, **z).expand(1, G, 1000).contiguous(), torch.full((1, G), 1000, **z), 16)
+    free = torch.empty((1, G, P), **z)
+    free[:, :, P - 1000:] = torch.arange(999, -1, -1, **z)        # the end of the list, where blocks come from
+    c = BlockCache(torch.empty((1, G, B, T), **z), torch.zeros((1, G, B), **z), free, torch.full((1, G), P, **z), 16)
     length = torch.zeros((1, G, B), **z)
     length[:, :, 254] = 16 * 900 + 3
     length[:, :, 255] = 16 * 20
@@ -225,14 +227,44 @@ def test_tables_beyond_32_bits():
     assert c.n_blocks[0, :, 254].tolist() == [901] * G and c.n_blocks[0, :, 255].tolist() == [20] * G
     assert torch.equal(c.table[0, :, 254, :901], torch.arange(901, **z).expand(G, 901))
     assert torch.equal(c.table[0, :, 255, :20], torch.arange(901, 921, **z).expand(G, 20))
-    cu, slots = torch.zeros((1, G, B + 1), **z), torch.zeros((1, G, 64), dtype=torch.int64, device=DEV)
+    cu, slots = torch.zeros((1, G, B + 1), **z), torch.empty((1, G, room), dtype=torch.int64, device=DEV)
     c.slot_map(length, cu, slots)
     assert slots[0, :, :2].tolist() == [[900 * 16 + 2, 921 * 16 - 1]] * G
-    o = [torch.zeros(s, **z) for s in ((1, G), (1, G, B), (1, G, B + 1), (1, G, 1000), (1, G, B))]
+    slots[:, :, 14723:14725] = -7
+    c.slot_map(length, cu, slots, n_new=length)
+    assert torch.equal(slots[0, :, :14403], torch.arange(14403, device=DEV).expand(G, 14403))
+    assert torch.equal(slots[0, :, 14403:14723], torch.arange(901 * 16, 921 * 16, device=DEV).expand(G, 320))
+    assert cu[0, :, -1].tolist() == [14723] * G and bool((slots[:, :, 14723:14725] == -7).all())
+    del slots
+    o = [torch.zeros(s, **z) for s in ((1, G), (1, G, B), (1, G, B + 1))] + [torch.empty((1, G, P), **z), torch.zeros((1, G, B), **z)]
     c.page_lists(length, *o)
     assert torch.equal(o[3][0, :, :921], torch.arange(921, **z).expand(G, 921)) and o[0].tolist() == [[2] * G]
+    c.free_list[:, :, P - 1000:] = -5
     c.block_tables(torch.zeros_like(length))
-    assert c.n_free.tolist() == [[1000] * G] and torch.equal(c.free_list[0, 0], torch.arange(999, -1, -1, **z))
+    assert c.n_free.tolist() == [[P] * G]
+    assert torch.equal(c.free_list[0, :, P - 921:], torch.arange(920, -1, -1, **z).expand(G, 921))
+    assert bool((c.free_list[:, :, P - 1000:P - 921] == -5).all())
+
+
+@pytest.mark.parametrize("N,G,B", [(3, 5, 40), (700, 8, 60), (1, 2, 256)])
+def test_workers_without_requests_and_requests_without_tokens(N, G, B):
+    p = Pair(N, G, B, 16, 300, 20, seed=2)
+    nothing = np.full((N, G, B), EMPTY, np.int32)
+    step = np.full(N, 7, np.int32)
+    some = nothing.copy()
+    some[:, ::2, B - 1] = 33                                      # every second worker runs one request, in its last slot
+    for length in (nothing, some, np.zeros_like(nothing), nothing - 0 * nothing, np.full_like(nothing, -7), some):
+        p.update(length, step)
+        p.slots(length, 3, step=step)
+        p.pages(length, step)
+        for q in (0, -4, 1, MOST):
+            p.slots(length, 50, np.full(nothing.shape, q, np.int32), step)
+    sparse = np.zeros_like(nothing)
+    sparse[:, :, [0, B // 2, B - 1]] = 9                          # new tokens in three slots of many running ones
+    full = np.full_like(nothing, 20)
+    p.update(full)
+    p.slots(full, 100, sparse)
+    p.pages(full)
 
 
 @pytest.mark.parametrize("shape", [(7, 3, 20, 8, 80, 30), (500, 10, 8, 8, 40, 12)])
