@@ -89,14 +89,14 @@ inline CacheShape cache_shape(int B, int workers, long long items, int limit)
     return s;
 }
 
-// ... and blocks a worker, by the same rule with pieces of 512 and of 2,048 items a warp, for calls that only copy: 146 million
+// ... and blocks a worker, by the same rule with pieces of 256 and of 2,048 items a warp, for calls that only copy: 146 million
 // prompt tokens of 256 workers 605 us with one block of eight warps each, 216 with 8, 200 with 18.
 inline CacheShape cache_copy_shape(int B, int workers, int items)
 {
     CacheShape s = cache_shape(B, workers, items, 8);
     if (s.warps > 1) {
         const long long warps = (long long)workers * s.warps;
-        const long long fill = std::min(kCacheWarps / warps, (long long)items / (512 * s.warps));
+        const long long fill = std::min(kCacheWarps / warps, (long long)items / (256 * s.warps));
         const long long even = std::min(4 * kCacheWarps / warps, (long long)items / (2048 * s.warps));
         s.slices = (int)std::max(1ll, std::max(fill, even));
     }
