@@ -304,7 +304,8 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
  * Each worker keeps its requests' keys and values in pool_blocks cache blocks of block_tokens tokens, numbered from 0.  Row b
  * of its block table names the blocks of the request in slot b, in token order; the blocks that no request holds are the
  * first n_free entries of its free list.  A new cache: n_blocks = 0, n_free = pool_blocks, free_list any order of the
- * blocks (fewer entries keep blocks out of use, e.g. one for padding).
+ * blocks (fewer entries keep blocks out of use, e.g. one for padding).  A block belongs to one request at most: rows that share
+ * blocks would give them back twice.
  *
  * All three calls read the tokens of each request from len [N][G][B]: len + step[i] with step [N], so that act_base and step
  * of br_worker_state serve as they are after br_step, or len itself with step NULL; BR_EMPTY_SLOT and sums below 1 are free
