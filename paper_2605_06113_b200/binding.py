@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libbr.so")
 
 BR_OK, BR_EINVAL, BR_ERANGE, BR_ECUDA, BR_ENOMEM, BR_ESTATE, BR_ELIMIT = 0, -1, -2, -3, -4, -5, -6
 STATIC_STAGE_BYTES = 8 << 20
+MAX_SLOT_ROOM = 1 << 30
 ST_QUEUE_OVERFLOW, ST_ITER_CAP, ST_BAD_STATE = 1, 2, 4
 EMPTY = -(2 ** 31)
 
@@ -373,6 +374,8 @@ class BlockCache:
         self.device = table.device
         self.N, self.G, self.B, self.columns = table.shape
         self.pool, self.block_tokens = free_list.shape[2], int(block_tokens)
+        if not all(-2 ** 31 <= v < 2 ** 31 for v in (self.pool, self.columns, self.block_tokens)):
+            raise ValueError("BlockCache: sizes are 32-bit numbers")
         self._fleet, self._worker, self._slot = (self.N,), (self.N, self.G), (self.N, self.G, self.B)
         self._cu = (self.N, self.G, self.B + 1)
         self._list = (*self._worker, self.pool)
@@ -394,7 +397,8 @@ class BlockCache:
                                    n_blocks.data_ptr(), self._free_list.data_ptr(), n_free.data_ptr())
 
     def commit(self, n_blocks, n_free):
-        """Takes the counts that an update wrote to other tensors as the cache's own (the old tensors are free again)."""
+        """Takes the counts that an update wrote to other tensors as the cache's own.  The old tensors are free again, but for
+        graphs captured with them."""
         self._refuse((n_blocks, "n_blocks", self._slot), (n_free, "n_free", self._worker))
         self._keep(n_blocks, n_free)
 
@@ -421,6 +425,8 @@ class BlockCache:
             N = self.N - first
         if first < 0 or N < 0 or first + N > self.N:
             raise ValueError(f"rows {first} to {first + N}: the cache has {self.N}")
+        if self._index < 0 and N:
+            raise ValueError(f"the cache is on {self.device}: the calls need tensors on a GPU")
         if stream is None:
             if self._index < 0:
                 stream = 0
@@ -469,6 +475,8 @@ class BlockCache:
                 (step is None or ok(step, self._fleet))):
             self._refuse((length, "length", slot), (cu, "cu", self._cu), (n_new, "n_new", slot), (step, "step", self._fleet))
         room = slots.shape[-1] if slots.dim() == 3 else -1
+        if room > MAX_SLOT_ROOM:
+            raise ValueError(f"slots: room for {room} tokens a worker; at most {MAX_SLOT_ROOM}")
         if slots.dtype is not self._int64 or slots.shape != (*self._worker, room) or slots.get_device() != self._index or \
                 not slots.is_contiguous():
             raise ValueError(f"slots: needs a contiguous int64 tensor [{self.N}, {self.G}, room] on {self.device}, "

@@ -107,6 +107,16 @@ def test_binding_refuses_tensors_of_another_type_shape_layout_or_device():
         cache.block_tables(length, short_blocks=torch.zeros((N, G, 1), **z), N=0)
     with pytest.raises(ValueError):
         cache.block_tables(length, n_free_out=torch.zeros((N, G), dtype=torch.int64), N=0)
+    for call in (lambda **k: cache.block_tables(length, **k), lambda **k: cache.slot_map(length, o["cu"], o["slots"], **k),
+                 lambda **k: cache.page_lists(length, *pages, **k)):
+        with pytest.raises(ValueError, match="on a GPU"):                        # host memory never reaches a kernel
+            call()
+        with pytest.raises(ValueError, match="on a GPU"):
+            call(N=1, first=1, stream=0)
+    with pytest.raises(ValueError, match="at most"):
+        cache.slot_map(length, o["cu"], torch.empty((N, G, 2 ** 32 + 5), dtype=torch.int64, device="meta"), N=0)
+    with pytest.raises(ValueError):
+        BlockCache(**{**good, "block_tokens": 2 ** 31})
     with pytest.raises(BrError):                                                 # no room for a single token
         cache.slot_map(length, o["cu"], torch.zeros((N, G, 0), dtype=torch.int64), N=0)
     with pytest.raises(BrError):
