@@ -342,6 +342,9 @@ __device__ __forceinline__ void cache_piece(int piece, int pieces, int count, in
 // free list from its end; the rest of those taken back joins the free list, the first on top.  What is read (the tails of
 // rows that shrink, the list below n_free) is never written by the same call, so the moves need no order.  The counts may be
 // written where they are read: a slot's by the thread that read it, the worker's after the whole team has read them.
+// 1,024 empty caches take 37.8 million blocks in 62 us, 0.70 of the measured copy bandwidth: what bounds it is the loads that
+// 48 registers a thread allow in flight (40 registers spill, 68 us; four loads a lane 72).  A burst that replaces a third of the
+// requests of 2,013 workers takes 11 us, by instructions and two trips to memory.
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs a)
 {
@@ -470,7 +473,9 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
     else move_items<true, false>(back_run, n_back, grow_run, 0, lo, hi, at.lane, table, list, top);
 }
 
-// One new token a request.
+// One new token a request: a thread reads the entry of each of its slots, its place is the number of running requests ahead.
+// Bound by memory, where an entry costs 64 bytes: 32,768 workers of 58 requests 29 us, 154 MB of DRAM at 0.82 of the measured copy
+// bandwidth; by the launch for single fleets, 2.3 us.
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
 {
@@ -530,7 +535,9 @@ __device__ __forceinline__ void store_four(FourSlots *p, const FourSlots &s)
 #endif
 }
 
-// Any number of new tokens: four in a row a lane, stored as 32 aligned bytes.
+// Any number of new tokens: four in a row a lane, which take one division and one or two entries, stored as 32 aligned bytes.
+// Bound by memory: 146 million prompt tokens 200 us, 1.17 GB at 0.90 of the measured copy bandwidth.  (Two groups of a lane at
+// once, warps that take the groups of a block in turn, and streaming stores all stay within 1 % of that.)
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
 {
@@ -619,7 +626,10 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
     }
 }
 
-// The running slots move up, their blocks follow one another.
+// The running slots move up, their blocks follow one another: item x of the worker is entry x of its list, and rows of 32 items are
+// read and written a line at a time.  Bound by memory for long requests, 37.8 million blocks 53 us at 0.82 of the measured copy
+// bandwidth, and by instructions for short ones, 2,107 workers with runs of 33 blocks 25 us.  (A lane that takes four blocks in a
+// row: 60 us and 26.6; a run at a time: 90 and 48.)
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256, 6) br_page_lists_kernel(const PageArgs a)
 {
