@@ -455,7 +455,8 @@ class BlockCache:
     def block_tables(self, length, n_blocks_out=None, n_free_out=None, short_blocks=None, step=None, N=None, first=0,
                      stream=None):
         """Brings tables and free lists in line with the lengths; the new counts go to ``n_blocks_out`` and ``n_free_out``
-        (default: the cache's own, in place).  With other tensors the cache stays as it was until ``commit`` takes them."""
+        (default: the cache's own, in place).  With other tensors the cache stays as it was until ``commit`` takes them.  One
+        of the two in place and the other elsewhere is refused with ValueError: the counts would not belong together."""
         nb = self.n_blocks if n_blocks_out is None else n_blocks_out
         nf = self.n_free if n_free_out is None else n_free_out
         ok, slot, worker = self._is, self._slot, self._worker
@@ -463,6 +464,9 @@ class BlockCache:
                 (short_blocks is None or ok(short_blocks, worker))):
             self._refuse((length, "length", slot), (nb, "n_blocks_out", slot), (nf, "n_free_out", worker),
                          (step, "step", self._fleet), (short_blocks, "short_blocks", worker))
+        if (n_blocks_out is not None or n_free_out is not None) and \
+                (nb.data_ptr() == self._n_blocks.data_ptr()) != (nf.data_ptr() == self._n_free.data_ptr()):
+            raise ValueError("n_blocks_out and n_free_out go together: both the cache's own or both other tensors")
         self._call("br_block_tables", self._batch(N, first, stream), self._packed, length.data_ptr(),
                    None if step is None else step.data_ptr(), nb.data_ptr(), nf.data_ptr(),
                    None if short_blocks is None else short_blocks.data_ptr())

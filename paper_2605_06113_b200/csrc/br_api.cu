@@ -878,6 +878,8 @@ int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const
     if (rc != BR_OK) return rc;
     if (!n_blocks_out || !n_free_out) return BR_EINVAL;
     if (misaligned(n_blocks_out, 4) || misaligned(n_free_out, 4) || misaligned(short_blocks, 4)) return BR_EINVAL;
+    // (one of the counts in place and the other elsewhere: the next update would deal out blocks that requests hold)
+    if ((n_blocks_out == cache->n_blocks) != (n_free_out == cache->n_free)) return BR_EINVAL;
     if (a.c.workers == 0) return BR_OK;
     a.n_blocks_out = n_blocks_out; a.n_free_out = n_free_out; a.short_out = short_blocks;
     const CacheKernels<br::TableArgs> k = BR_CACHE_KERNELS(br_block_tables_kernel);

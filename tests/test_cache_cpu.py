@@ -186,3 +186,30 @@ def test_definition_undoes_what_it_did():
         assert [f.table[0, 0, b, :n].tolist() for b, n in enumerate(f.n_blocks[0, 0])] == before[2]
         assert f.free_list[0, 0, :f.n_free[0, 0]].tolist() == before[3]
     f.check_partition()
+
+
+def test_count_outputs_go_together():
+    """Counts in place for one array and elsewhere for the other would leave a cache whose n_blocks and n_free disagree."""
+    some = BrInstanceBatch(n_instances=0, first_instance=0, n_steps=1, stream=None)
+    c = _cache(n_blocks=FAKE, n_free=2 * FAKE)
+    L = binding.lib()
+    for nb, nf, want in ((FAKE, 2 * FAKE, BR_OK), (3 * FAKE, 4 * FAKE, BR_OK), (FAKE, 4 * FAKE, BR_EINVAL), (3 * FAKE, 2 * FAKE, BR_EINVAL)):
+        assert L.br_block_tables(C.byref(some), C.byref(c), FAKE, None, nb, nf, None) == want, (nb, nf)
+    cache = BlockCache.empty(2, 3, 4, 16, 5, 6, device="cpu")
+    length, nb, nf = torch.zeros_like(cache.n_blocks), torch.empty_like(cache.n_blocks), torch.empty_like(cache.n_free)
+    for mixed in (dict(n_blocks_out=nb), dict(n_free_out=nf), dict(n_blocks_out=cache.n_blocks, n_free_out=nf),
+                  dict(n_blocks_out=nb, n_free_out=cache.n_free)):
+        with pytest.raises(ValueError, match="go together"):
+            cache.block_tables(length, N=0, **mixed)
+    for both in (dict(), dict(n_blocks_out=nb, n_free_out=nf), dict(n_blocks_out=cache.n_blocks, n_free_out=cache.n_free),
+                 dict(n_blocks_out=cache.n_blocks), dict(n_free_out=cache.n_free)):
+        cache.block_tables(length, N=0, **both)
+
+
+def test_definition_with_one_of_the_counts_in_place_deals_blocks_out_twice():
+    """Why they go together: with entries kept out of use nothing notices, and two requests share blocks."""
+    f = ref.Fleets(1, 1, 2, t=1, P=10, T=4)
+    f.n_free[:] = 4                                                              # blocks 9 to 6; the others are out of use
+    f.n_blocks = f.update(np.array([[[2, 0]]], np.int32), commit=False)[0]       # (beside the old n_free)
+    assert f.update(np.array([[[2, 2]]], np.int32))[2][0, 0] == 0
+    assert f.table[0, 0, 0].tolist()[:2] == f.table[0, 0, 1].tolist()[:2] == [6, 7]
