@@ -340,7 +340,8 @@ typedef struct {
  *   n_blocks_out [N][G][B], n_free_out [N][G]   the counts after the update: cache->n_blocks and cache->n_free themselves, or
  *                  two other arrays (BR_EINVAL for one of each: counts that do not belong together deal blocks out twice).
  *                  With other arrays the old counts stay valid: the entries they reach are not written, so that an update
- *                  can be looked at and dropped.
+ *                  can be looked at and dropped.  Rows outside the batch are not written: before such arrays take the
+ *                  place of the cache's they have to hold its counts there.
  *   short_blocks   [N][G] blocks that requests of the worker still lack (2^31 - 1 if more); -1 if the worker's counts cannot
  *                  be (outside their ranges, or more blocks held and free than the pool has), which leaves it as it was;
  *                  may be NULL

@@ -397,8 +397,9 @@ class BlockCache:
                                    n_blocks.data_ptr(), self._free_list.data_ptr(), n_free.data_ptr())
 
     def commit(self, n_blocks, n_free):
-        """Takes the counts that an update wrote to other tensors as the cache's own.  The old tensors are free again, but for
-        graphs captured with them."""
+        """Takes the counts that an update wrote to other tensors as the cache's own, all rows of them: those outside the
+        update's ``first`` to ``first + N`` were not written and have to hold the cache's counts already (copy them in
+        ahead of such an update).  The old tensors are free again, but for graphs captured with them."""
         self._refuse((n_blocks, "n_blocks", self._slot), (n_free, "n_free", self._worker))
         self._keep(n_blocks, n_free)
 
@@ -455,8 +456,9 @@ class BlockCache:
     def block_tables(self, length, n_blocks_out=None, n_free_out=None, short_blocks=None, step=None, N=None, first=0,
                      stream=None):
         """Brings tables and free lists in line with the lengths; the new counts go to ``n_blocks_out`` and ``n_free_out``
-        (default: the cache's own, in place).  With other tensors the cache stays as it was until ``commit`` takes them.  One
-        of the two in place and the other elsewhere is refused with ValueError: the counts would not belong together."""
+        (default: the cache's own, in place), rows ``first`` to ``first + N`` of them.  With other tensors the cache stays as
+        it was until ``commit`` takes them, which takes all rows.  One of the two in place and the other elsewhere is refused
+        with ValueError: the counts would not belong together."""
         nb = self.n_blocks if n_blocks_out is None else n_blocks_out
         nf = self.n_free if n_free_out is None else n_free_out
         ok, slot, worker = self._is, self._slot, self._worker

@@ -448,3 +448,27 @@ def test_range_checked_build():
         assert binding.lib().br_debug_bounds_hits() == hits
     finally:
         binding.use_library(None)
+
+
+@pytest.mark.parametrize("shape", [(7, 3, 20, 8, 80, 30), (500, 10, 8, 8, 40, 12)])
+def test_rows_of_a_batch_updated_elsewhere_and_committed(shape):
+    p = Pair(*shape, seed=19)
+    f = p.f
+    rng = np.random.default_rng(8)
+    n = rng.integers(0, 60, (f.N, f.G, f.B)).astype(np.int32)
+    p.update(n)
+    for first, N in ((2, 3), (0, 1), (f.N - 1, 1), (4, f.N - 4)):
+        n = (_walk(rng, f, n.astype(np.int64), 0.3, 0.6, 5)).astype(np.int32)
+        spare = (p.c.n_blocks.clone(), p.c.n_free.clone())        # rows outside the update hold the cache's counts
+        p.c.block_tables(_gpu(n), *spare, first=first, N=N)
+        wnb, wnf, _ = f.update(n, first=first, N=N, commit=False)
+        p.same((spare[0], wnb), (spare[1], wnf))
+        p.same()                                                  # not taken yet
+        p.c.commit(*spare)
+        f.n_blocks, f.n_free = wnb, wnf
+        p.same()
+    rows = (torch.full_like(p.c.n_blocks, -77), torch.full_like(p.c.n_free, -77))
+    p.c.block_tables(_gpu(n), *rows, first=1, N=2)
+    for t in rows:                                                # rows outside the update are left as they were
+        assert bool((t[:1] == -77).all()) and bool((t[3:] == -77).all()) and not bool((t[1:3] == -77).any())
+    f.check_partition()
