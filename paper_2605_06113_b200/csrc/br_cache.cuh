@@ -441,7 +441,8 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
         const bool fits_row = need[i] <= c.T;
         const int upto = sum.y + (fits_row ? more : 0);
         const bool served = fits_row && upto <= n_free + R;
-        if (more > 0 && fits_row) grow_run[grow_rank++] = {served ? upto : sum.y, (at.slot + i) * c.T + have[i] - sum.y};
+        // (the runs of requests that are not served lie behind A, the end of what is moved)
+        if (more > 0 && fits_row) grow_run[grow_rank++] = {upto, (at.slot + i) * c.T + have[i] - sum.y};
         sum.y = upto;
         if (served) A = upto;
         want += more;

@@ -472,3 +472,26 @@ def test_rows_of_a_batch_updated_elsewhere_and_committed(shape):
     for t in rows:                                                # rows outside the update are left as they were
         assert bool((t[:1] == -77).all()) and bool((t[3:] == -77).all()) and not bool((t[1:3] == -77).any())
     f.check_partition()
+
+
+@pytest.mark.parametrize("N,G,end", [(2, 3, 255), (2, 3, 256), (2, 3, 257), (2, 3, 512), (600, 8, 256)])
+def test_grants_that_end_at_a_window_with_requests_behind_them_unserved(N, G, end):
+    """The last block granted is the last of a window of 256 (or beside it), and what follows asks for a block each, or for many:
+    served from the free list, from blocks taken back, and from both."""
+    B, T = 28, 700
+    sizes = [end - 26, 1, 1, 3, 2, 1, 1, 2, 7, 8]                  # ten requests that take `end` blocks
+    behind = [1, 1, 2, 1, 300, 1, 1, 40]                           # nothing is left for these
+    after = np.array(sizes + [0] * 4 + behind + [0] * 6, np.int32)
+    for before in ([0] * 28,                                       # all from the free list
+                   [0] * 22 + [end - 9, 2, 3, 2, 1, 1],            # all of them taken back
+                   [0] * 22 + [end - 130, 2, 3, 2, 1, 1],          # some of them
+                   [0] * 10 + [end - 9, 2, 3, 2] + [0] * 8 + [1, 1] + [0] * 4):
+        p = Pair(N, G, B, 1, end, T, seed=end)
+        p.update(np.tile(np.array(before, np.int32), (N, G, 1)))
+        n = np.tile(after, (N, G, 1))
+        assert (p.update(n, out=True) == sum(behind)).all()
+        assert (p.update(n) == sum(behind)).all() and not p.f.n_free.any()
+        p.pages(n)
+        n[:, :, 0] = 0                                             # and the others get what comes back
+        p.update(n)
+    p.f.check_partition()
