@@ -364,7 +364,8 @@ class BlockCache:
     one device, contiguous, owned by the caller; ``block_tokens`` is the size of a cache block.  ``BlockCache.empty`` makes
     the tensors of a new cache.  Every call takes the request lengths [N, G, B] as int32, plain or, with ``step`` [N], as the
     router keeps them (``st["act_base"], step=st["step"]``), and works on the rows ``first`` to ``first + N``.  A tensor of
-    another type, shape, layout or device is refused with ValueError."""
+    another type, shape, layout or device is refused with ValueError.  Calls use the memory that the cache's tensors have
+    when they are made (a captured graph that of its capture)."""
 
     def __init__(self, table, n_blocks, free_list, n_free, block_tokens):
         import torch
@@ -379,22 +380,33 @@ class BlockCache:
         self._fleet, self._worker, self._slot = (self.N,), (self.N, self.G), (self.N, self.G, self.B)
         self._cu = (self.N, self.G, self.B + 1)
         self._list = (*self._worker, self.pool)
-        self._refuse((table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
-                     (free_list, "free_list", self._list), (n_free, "n_free", self._worker))
         self._table, self._free_list = table, free_list
-        self._keep(n_blocks, n_free)
         self._index = table.get_device()                     # -1: not on a GPU
-        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._take(n_blocks, n_free)
+        self._whole = None, b""
+        if self._index < 0:
+            self._current_stream = lambda index: 0
+        else:
+            self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        # (with one GPU it is the current one)
+        self._several = self._index >= 0 and torch.cuda.device_count() > 1
         self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
     # (read-only: the calls use the tensors that the handle was made with, or the counts of the last commit)
     table, free_list = property(lambda self: self._table), property(lambda self: self._free_list)
     n_blocks, n_free = property(lambda self: self._n_blocks), property(lambda self: self._n_free)
 
+    def _take(self, n_blocks, n_free):
+        self._refuse((self._table, "table", (*self._slot, self.columns)), (n_blocks, "n_blocks", self._slot),
+                     (self._free_list, "free_list", self._list), (n_free, "n_free", self._worker))
+        self._keep(n_blocks, n_free)
+
     def _keep(self, n_blocks, n_free):
         self._n_blocks, self._n_free = n_blocks, n_free
-        self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, self._table.data_ptr(),
-                                   n_blocks.data_ptr(), self._free_list.data_ptr(), n_free.data_ptr())
+        self._addresses = self._table.data_ptr, n_blocks.data_ptr, self._free_list.data_ptr, n_free.data_ptr
+        self._at = tuple(address() for address in self._addresses)
+        self._packed = _pack_cache(self.G, self.B, self.block_tokens, self.pool, self.columns, *self._at)
 
     def commit(self, n_blocks, n_free):
         """Takes the counts that an update wrote to other tensors as the cache's own, all rows of them: those outside the
@@ -422,34 +434,41 @@ class BlockCache:
                                  f"got {t.dtype} {list(t.shape)} on {t.device}")
 
     def _batch(self, N, first, stream):
-        if N is None:
-            N = self.N - first
-        if first < 0 or N < 0 or first + N > self.N:
-            raise ValueError(f"rows {first} to {first + N}: the cache has {self.N}")
+        table, n_blocks, free_list, n_free = self._addresses
+        if (table(), n_blocks(), free_list(), n_free()) != self._at:             # a tensor of the cache was given other memory
+            self._take(self._n_blocks, self._n_free)
+        whole = N is None and first == 0
+        if whole:
+            N = self.N
+        else:
+            if N is None:
+                N = self.N - first
+            if first < 0 or N < 0 or first + N > self.N:
+                raise ValueError(f"rows {first} to {first + N}: the cache has {self.N}")
         if self._index < 0 and N:
             raise ValueError(f"the cache is on {self.device}: the calls need tensors on a GPU")
         if stream is None:
-            if self._index < 0:
-                stream = 0
-            elif self._raw_stream is not None:
-                stream = self._raw_stream(self._index)
-            else:
-                stream = self.torch.cuda.current_stream(self.device).cuda_stream
+            stream = self._current_stream(self._index)
         elif isinstance(stream, C.c_void_p):
             stream = stream.value or 0
         elif hasattr(stream, "cuda_stream"):
             stream = stream.cuda_stream
-        return _pack_batch(N, first, 1, stream)
+        if not whole:
+            return _pack_batch(N, first, 1, stream)
+        packed = self._whole                                 # the batch of all rows on the stream of the last call
+        if packed[0] != stream:
+            packed = self._whole = stream, _pack_batch(N, 0, 1, stream)
+        return packed[1]
 
-    def _call(self, name, *args):
+    def _call(self, name, batch, *args):
         if self.N == 0:
             return                                           # (empty tensors have no address)
-        fn = getattr(lib(), name)
-        if self._index >= 0 and self._current_device() != self._index:
+        fn = getattr(_lib or lib(), name)
+        if self._several and self._current_device() != self._index:
             with self.torch.cuda.device(self.device):       # the launch goes to the tensors' device
-                rc = fn(*args)
+                rc = fn(batch, self._packed, *args)
         else:
-            rc = fn(*args)
+            rc = fn(batch, self._packed, *args)
         if rc != BR_OK:
             raise BrError(rc, name)
 
@@ -459,18 +478,19 @@ class BlockCache:
         (default: the cache's own, in place), rows ``first`` to ``first + N`` of them.  With other tensors the cache stays as
         it was until ``commit`` takes them, which takes all rows.  One of the two in place and the other elsewhere is refused
         with ValueError: the counts would not belong together."""
-        nb = self.n_blocks if n_blocks_out is None else n_blocks_out
-        nf = self.n_free if n_free_out is None else n_free_out
+        nb = self._n_blocks if n_blocks_out is None else n_blocks_out
+        nf = self._n_free if n_free_out is None else n_free_out
         ok, slot, worker = self._is, self._slot, self._worker
         if not (ok(length, slot) and ok(nb, slot) and ok(nf, worker) and (step is None or ok(step, self._fleet)) and
                 (short_blocks is None or ok(short_blocks, worker))):
             self._refuse((length, "length", slot), (nb, "n_blocks_out", slot), (nf, "n_free_out", worker),
                          (step, "step", self._fleet), (short_blocks, "short_blocks", worker))
-        if (n_blocks_out is not None or n_free_out is not None) and \
-                (nb.data_ptr() == self._n_blocks.data_ptr()) != (nf.data_ptr() == self._n_free.data_ptr()):
+        batch, at = self._batch(N, first, stream), self._at
+        nb = at[1] if n_blocks_out is None else nb.data_ptr()
+        nf = at[3] if n_free_out is None else nf.data_ptr()
+        if (nb == at[1]) != (nf == at[3]):
             raise ValueError("n_blocks_out and n_free_out go together: both the cache's own or both other tensors")
-        self._call("br_block_tables", self._batch(N, first, stream), self._packed, length.data_ptr(),
-                   None if step is None else step.data_ptr(), nb.data_ptr(), nf.data_ptr(),
+        self._call("br_block_tables", batch, length.data_ptr(), None if step is None else step.data_ptr(), nb, nf,
                    None if short_blocks is None else short_blocks.data_ptr())
 
     def slot_map(self, length, cu, slots, n_new=None, step=None, N=None, first=0, stream=None):
@@ -480,14 +500,15 @@ class BlockCache:
         if not (ok(length, slot) and ok(cu, self._cu) and (n_new is None or ok(n_new, slot)) and
                 (step is None or ok(step, self._fleet))):
             self._refuse((length, "length", slot), (cu, "cu", self._cu), (n_new, "n_new", slot), (step, "step", self._fleet))
-        room = slots.shape[-1] if slots.dim() == 3 else -1
+        shape = slots.shape
+        room = shape[2] if len(shape) == 3 else -1
         if room > MAX_SLOT_ROOM:
             raise ValueError(f"slots: room for {room} tokens a worker; at most {MAX_SLOT_ROOM}")
-        if slots.dtype is not self._int64 or slots.shape != (*self._worker, room) or slots.get_device() != self._index or \
+        if slots.dtype is not self._int64 or shape != (self.N, self.G, room) or slots.get_device() != self._index or \
                 not slots.is_contiguous():
             raise ValueError(f"slots: needs a contiguous int64 tensor [{self.N}, {self.G}, room] on {self.device}, "
                              f"got {slots.dtype} {list(slots.shape)} on {slots.device}")
-        self._call("br_slot_map", self._batch(N, first, stream), self._packed, length.data_ptr(),
+        self._call("br_slot_map", self._batch(N, first, stream), length.data_ptr(),
                    None if step is None else step.data_ptr(), None if n_new is None else n_new.data_ptr(), room,
                    cu.data_ptr(), slots.data_ptr())
 
@@ -499,7 +520,7 @@ class BlockCache:
             self._refuse((length, "length", slot), (n_seq, "n_seq", self._worker), (seq_slot, "seq_slot", slot),
                          (indptr, "indptr", self._cu), (indices, "indices", self._list), (last_tokens, "last_tokens", slot),
                          (step, "step", self._fleet))
-        self._call("br_page_lists", self._batch(N, first, stream), self._packed, length.data_ptr(),
+        self._call("br_page_lists", self._batch(N, first, stream), length.data_ptr(),
                    None if step is None else step.data_ptr(), n_seq.data_ptr(), seq_slot.data_ptr(), indptr.data_ptr(),
                    indices.data_ptr(), last_tokens.data_ptr())
 

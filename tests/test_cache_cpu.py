@@ -213,3 +213,37 @@ def test_definition_with_one_of_the_counts_in_place_deals_blocks_out_twice():
     f.n_blocks = f.update(np.array([[[2, 0]]], np.int32), commit=False)[0]       # (beside the old n_free)
     assert f.update(np.array([[[2, 2]]], np.int32))[2][0, 0] == 0
     assert f.table[0, 0, 0].tolist()[:2] == f.table[0, 0, 1].tolist()[:2] == [6, 7]
+
+
+def test_calls_use_the_memory_that_the_tensors_have_now(monkeypatch):
+    """A tensor of the cache may be given other memory after the handle was made (resized, reloaded, moved into a pool)."""
+    N, G, B, T, P = 2, 3, 4, 6, 5
+    cache = BlockCache.empty(N, G, B, 16, P, T, device="cpu")
+    length, o = torch.zeros_like(cache.n_blocks), _buffers(N, G, B, P)
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda batch, packed, *args: seen.append(BrBlockCache.from_buffer_copy(packed)) or BR_OK
+
+    monkeypatch.setattr(binding, "_lib", Library())
+    calls = (lambda: cache.block_tables(length, N=0), lambda: cache.slot_map(length, o["cu"], o["slots"], N=0),
+             lambda: cache.page_lists(length, o["n_seq"], o["seq_slot"], o["indptr"], o["indices"], o["last_tokens"], N=0))
+    names = ("table", "n_blocks", "free_list", "n_free")
+    for name in names:
+        held = getattr(cache, name)
+        for change in (lambda: held.set_(held.clone()), lambda: setattr(held, "data", held.data.clone())):
+            old = held.data_ptr()
+            keep = held.untyped_storage()                                        # (so that the new memory is elsewhere)
+            change()
+            assert held.data_ptr() != old and keep.data_ptr() == old
+            for call in calls:
+                call()
+                assert [getattr(seen[-1], n) for n in names] == [getattr(cache, n).data_ptr() for n in names], name
+                assert (seen[-1].G, seen[-1].B, seen[-1].block_tokens, seen[-1].pool_blocks, seen[-1].table_blocks) == (G, B, 16, P, T)
+    count = len(seen)
+    cache.free_list.data = torch.zeros((N, G, P - 1), dtype=torch.int32)
+    for call in calls:
+        with pytest.raises(ValueError, match="free_list"):
+            call()
+    assert len(seen) == count
