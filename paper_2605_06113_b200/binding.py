@@ -374,7 +374,13 @@ class BlockCache:
             raise ValueError("BlockCache: table is [N, G, B, columns] and free_list [N, G, pool]")
         self.device = table.device
         self.N, self.G, self.B, self.columns = table.shape
-        self.pool, self.block_tokens = free_list.shape[2], int(block_tokens)
+        try:
+            whole = int(block_tokens)
+        except (TypeError, ValueError, OverflowError):
+            whole = None
+        if whole != block_tokens or whole is None:
+            raise ValueError(f"block_tokens: needs a whole number of tokens, got {block_tokens!r}")
+        self.pool, self.block_tokens = free_list.shape[2], whole
         if not all(-2 ** 31 <= v < 2 ** 31 for v in (self.pool, self.columns, self.block_tokens)):
             raise ValueError("BlockCache: sizes are 32-bit numbers")
         self._fleet, self._worker, self._slot = (self.N,), (self.N, self.G), (self.N, self.G, self.B)

@@ -247,3 +247,13 @@ def test_calls_use_the_memory_that_the_tensors_have_now(monkeypatch):
         with pytest.raises(ValueError, match="free_list"):
             call()
     assert len(seen) == count
+
+
+def test_block_size_is_a_whole_number():
+    c = BlockCache.empty(2, 3, 4, 16, 5, 6, device="cpu")
+    arrays = (c.table, c.n_blocks, c.free_list, c.n_free)
+    for t in (16.5, 0.99, float("nan"), float("inf"), "16", None):
+        with pytest.raises(ValueError, match="block_tokens"):
+            BlockCache(*arrays, t)
+    for t in (16, 16.0, np.int64(16), torch.tensor(16)):
+        assert BlockCache(*arrays, t).block_tokens == 16
