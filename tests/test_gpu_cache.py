@@ -495,3 +495,32 @@ def test_grants_that_end_at_a_window_with_requests_behind_them_unserved(N, G, en
         n[:, :, 0] = 0                                             # and the others get what comes back
         p.update(n)
     p.f.check_partition()
+
+
+def test_a_worker_without_free_blocks_is_not_chosen():
+    """n_free as br_fscore's cap: the worker that the scores favour is chosen without it, the best of the others with it."""
+    cfg = wlm.get_config("c0")
+    r = Router(wlm.make_workload(cfg, n_instances=2), device=DEV)
+    G = cfg.G
+    c = r.block_cache(2, 16, 30, 40)
+    z = dict(dtype=torch.int32, device=DEV)
+    s = torch.tensor([[100, 700, 1, 5000]] * 2, **z)
+    F = torch.full((2, 4, G), float("nan"), dtype=torch.float64, device=DEV)
+    Lh = torch.randint(0, 10 ** 6, (2, G), dtype=torch.int64, device=DEV, generator=torch.Generator(DEV).manual_seed(3))
+    length = torch.zeros((2, G, cfg.B), **z)
+    best = torch.full((2, 4), -1, **z)
+    r.fscore(s, Lh, F, cap=c.n_free, best_g=best)
+    assert torch.equal(best.long(), F.argmax(-1)) and not bool(F.isnan().any())
+    favoured = best.clone()
+    for i, g in enumerate(best[:, 0].tolist()):
+        length[i, g, 5] = 30 * 16                                 # one request takes the worker's whole pool
+    c.block_tables(length)
+    assert (c.n_free == 0).sum() == 2
+    best.fill_(-1)
+    r.fscore(s, Lh, F, best_g=best)
+    assert torch.equal(best, favoured)
+    best.fill_(-1)
+    r.fscore(s, Lh, F, cap=c.n_free, best_g=best)
+    assert torch.equal(best.long(), F.masked_fill((c.n_free == 0)[:, None, :], -float("inf")).argmax(-1))
+    assert bool((best[:, 0] != favoured[:, 0]).all())
+    r.close()
