@@ -312,7 +312,8 @@ int br_survival_chat(br_ctx *ctx, void *stream, const int32_t *hist_sorted, cons
  * slots, sums beyond 2^31 - 1 count as that.  Device pointers aligned to their type; asynchronous on batch.stream, whose
  * device must be current; batch.n_steps is not used.  BR_EINVAL for null or misaligned pointers, sizes outside the limits and
  * (first_instance + n_instances) * G beyond 2^31 - 1; BR_ECUDA if the launch failed.  No context is needed and nothing
- * allocated; calls on different rows may overlap, and all may be captured into graphs.
+ * allocated; calls on different rows may overlap, and all may be captured into graphs.  What a call writes overlaps neither
+ * what it reads nor its other outputs, but for the counts that br_block_tables updates in place.
  */
 #define BR_MAX_BLOCK_TOKENS (1 << 20)
 #define BR_MAX_TABLE_BLOCKS (1 << 22)
@@ -366,7 +367,8 @@ int br_slot_map(const br_instance_batch *batch, const br_block_cache *cache, con
  *   n_seq       [N][G]         running requests
  *   seq_slot    [N][G][B]      the slot of each, -1 from n_seq on
  *   indptr      [N][G][B + 1]  the blocks of request r are indices[indptr[r] .. indptr[r + 1]); rows from n_seq on are empty
- *   indices     [N][G][pool_blocks]  block numbers; entries from indptr[B] on are left as they were
+ *   indices     [N][G][pool_blocks]  block numbers; entries from indptr[B] on are left as they were, and blocks from
+ *                              pool_blocks on dropped (only counts that cannot be list that many)
  *   last_tokens [N][G][B]      tokens in the last of its blocks (0 without one, and from n_seq on)
  * A request that holds fewer blocks than its tokens need is listed with what it holds, all of it full; one that holds more
  * with what it needs.  The table is not written.

@@ -883,8 +883,8 @@ int br_block_tables(const br_instance_batch *batch, br_block_cache *cache, const
     if (a.c.workers == 0) return BR_OK;
     a.n_blocks_out = n_blocks_out; a.n_free_out = n_free_out; a.short_out = short_blocks;
     const CacheKernels<br::TableArgs> k = BR_CACHE_KERNELS(br_block_tables_kernel);
-    // (What an update moves is not known here, mostly next to nothing: the warps that the GPU holds at once, eight a worker at
-    // most, and one block a worker, since more would have to meet before the counts are written.)
+    // (What an update moves is not known here, mostly next to nothing: the warps of one round, eight a worker at most, and one
+    // block a worker, since more would have to meet before the counts are written.)
     const int some = 256 * 8 + 1;
     return launch_cache(k, a, br::cache_shape(cache->B, a.c.workers, some, 8), batch, "br_block_tables launch");
 }

@@ -9,14 +9,13 @@
 // Prefix sums over a worker's slots turn each of them into independent copies: every moved block, token or page knows its
 // source and its place from the sums alone, so nothing is ordered by atomics and results do not depend on timing.
 //
-// A team of warps takes one worker: a single warp where there are workers enough to fill the GPU (eight of them a block), a
-// block otherwise.  Each thread owns one or two slots, and one exchange of the warps' sums gives every slot its place.  What
-// is to be moved is then cut into equal pieces by items, not by slots, so one long request is spread like many short ones.
+// A team of warps takes one worker: a single warp where there are many workers (eight of them a block), a block otherwise.  Each
+// thread owns one or two slots, and one exchange of the warps' sums gives every slot its place.  What is to be moved is then cut
+// into equal pieces by items, not by slots, so one long request is spread like many short ones.
 //
-// Large calls are bound by memory: 16 of the largest fleets' page lists (37.8 million blocks) take 53.9 us, 0.81 of the
-// measured copy bandwidth, 146 million prompt tokens 200 us, 0.90.  Calls between two decode steps move next to nothing and
-// are bound by the launch and two trips to memory: 2.0 us for four workers, 6.5 us for 8,192, a tenth of which take a prompt.
-// (Device times of captured calls.)
+// Large calls are bound by memory: 16 of the largest fleets' page lists (37.8 million blocks) take 53.5 us, 0.82 of the
+// measured copy bandwidth, 146 million prompt tokens 201 us, 0.90.  Calls between two decode steps move next to nothing: 2.0 us
+// for four workers, the launch, 6.5 us for 8,192, a tenth of which take a prompt.  (Device times of captured calls, here and below.)
 #pragma once
 #include <algorithm>
 #include "br_device.cuh"
@@ -26,7 +25,12 @@ namespace br {
 
 constexpr int kCacheTeams = 8;              // single-warp teams of a block
 constexpr int kMoves = 8;                   // items of a lane on their way at once
-constexpr int kCacheWarps = 148 * 64;       // the warps that the GPU holds at once
+// The warps of a launch that the rules below count as one round: all that 148 SMs have room for, 64 each.  Registers allow that
+// in the slot kernels of whole blocks only (27 to 31 a thread); single-warp teams of slot maps (39) and page lists (40) hold 48
+// warps an SM, block tables (48) 40, so that a round is up to 1.6 waves of theirs.  Counting 40 instead does not pay: 1,024 empty
+// caches 67.2 us with four warps a worker, all of them resident, 61.9 with eight; page lists of 37.8 million blocks 55.0, 53.4; a
+// third of the requests of 2,013 workers replaced 10.1 us with two warps, 11.0 with four, but 12.9 and 11.1 if not captured.
+constexpr int kCacheWarps = 148 * 64;
 
 // x / d = umulhi(2 x, magic) >> shift for 0 <= x < 2^31, 1 <= d <= 2^31 - 1: with s = ceil(log2 d) and
 // m = ceil(2^(31 + s) / d) <= 2^32 - 1 (d no power of two) the error m d - 2^(31 + s) is below d <= 2^s, so
@@ -72,11 +76,10 @@ struct PageArgs {
 // The team of a worker, how many slots a thread of it owns (one or two), and how many blocks share the worker.
 struct CacheShape { int warps, spl, slices; };
 
-// Warps a worker for calls that move up to `items` items of it, at most `limit`: more while all of them are on the GPU at once
-// and each has more than 256 items, or up to four rounds of them while each has 2,048 or more, which evens out workers that
-// move different amounts.  (Page lists of 8,192 workers of 130 requests' blocks each: 112 us with one warp a worker, 98 with
-// four; chunks of their prompts 238, 179; page lists of 2,107 workers of up to 9,999 blocks 25 us with four warps in one round,
-// 33 in two.)
+// Warps a worker for calls that move up to `items` items of it, at most `limit`: more while they stay within a round and each
+// has more than 256 items, or up to four rounds of them while each has 2,048 or more, which evens out workers that move
+// different amounts.  (8,192 workers with pools of 10,240 blocks: page lists 49.5 us with one warp a worker, 48.0 with two, 46.2
+// with four, the rule's choice, 54.8 with eight.  Chunks of their prompts, room for 12,345 tokens: 119, 85.1, 84.7, 86.5.)
 inline CacheShape cache_shape(int B, int workers, long long items, int limit)
 {
     CacheShape s = {1, 1, 1};
@@ -90,7 +93,8 @@ inline CacheShape cache_shape(int B, int workers, long long items, int limit)
 }
 
 // ... and blocks a worker, by the same rule with pieces of 256 and of 2,048 items a warp, for calls that only copy: 146 million
-// prompt tokens of 256 workers 605 us with one block of eight warps each, 216 with 8, 200 with 18.
+// prompt tokens of 256 workers 396 us with one block of eight warps each, 216 with 8, 201 with 18, the rule's choice; chunks of 264
+// workers 9.7 with one, 8.2 with four, the rule's choice, 9.8 with 8.
 inline CacheShape cache_copy_shape(int B, int workers, int items)
 {
     CacheShape s = cache_shape(B, workers, items, 8);
@@ -232,8 +236,8 @@ template <typename Out> struct UpList {
 // The runs of the items of one warp, window by window of kMoves rows of 32.  Where one run covers a window, the rule for long
 // requests, its items are a constant apart; up to three starts are compared with every item; with more of them a bit for each
 // item that starts a run turns into the run of every item by counting bits, which has no loop that lanes leave one by one.  No
-// run is empty.  (Lanes that walk through the runs one by one: page lists of 2,107 workers with runs of 33 blocks 29.5 us, 25.1
-// this way; windows of 128 items: filling 1,024 caches 80.6 us, 62 with 256.)
+// run is empty.  (Lanes that walk through the runs one by one: page lists of 2,107 workers with runs of 33 blocks 29.5 us, 24.7
+// this way; windows of 128 items, four loads a lane: 29.5, and filling 1,024 caches 79.4 us, 61.9 with 256.)
 struct Windows {
     const Run *runs;
     int n, run;                             // run: that of the window's first item
@@ -284,7 +288,7 @@ struct Windows {
 };
 
 // An entry with few others of interest near it: 64 bytes of memory are fetched for it, not the usual 128 (newest tokens of
-// 32,768 workers' requests: 43.1 us with plain loads, 28.7 this way; 259 MB read from DRAM, 138).
+// 32,768 workers' requests: 43.1 us with plain loads, 29.1 this way; 259 MB read from DRAM, 138).
 __device__ __forceinline__ int lone_entry(const int32_t *p)
 {
     int v;
@@ -342,9 +346,11 @@ __device__ __forceinline__ void cache_piece(int piece, int pieces, int count, in
 // free list from its end; the rest of those taken back joins the free list, the first on top.  What is read (the tails of
 // rows that shrink, the list below n_free) is never written by the same call, so the moves need no order.  The counts may be
 // written where they are read: a slot's by the thread that read it, the worker's after the whole team has read them.
-// 1,024 empty caches take 37.8 million blocks in 62 us, 0.70 of the measured copy bandwidth: what bounds it is the loads that
-// 48 registers a thread allow in flight (40 registers spill, 68 us; four loads a lane 72).  A burst that replaces a third of the
-// requests of 2,013 workers takes 11 us, by instructions and two trips to memory.
+// 1,024 empty caches take 37.8 million blocks in 61.9 us, 0.70 of the measured copy bandwidth.  48 registers a thread leave 40
+// warps an SM, with eight loads a lane in flight: the launch of 1,024 blocks is a full wave of 740 and a partial second one.
+// (40 registers spill, 66.8 us; four loads a lane 79.4.)  A burst that replaces a third of the requests of 2,013 workers takes 11.0 us,
+// in 1.36 waves, by instructions (0.6 of the issue slots) and two trips to memory.  A decode step of 8,192 workers takes 6.5 us, in
+// 1.38 waves: 3.6 where nothing moves, 4.5 with a block a request at most.
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs a)
 {
@@ -475,8 +481,8 @@ __global__ void __launch_bounds__(256, 5) br_block_tables_kernel(const TableArgs
 }
 
 // One new token a request: a thread reads the entry of each of its slots, its place is the number of running requests ahead.
-// Bound by memory, where an entry costs 64 bytes: 32,768 workers of 58 requests 29 us, 154 MB of DRAM at 0.82 of the measured copy
-// bandwidth; by the launch for single fleets, 2.3 us.
+// Bound by memory, where an entry costs 64 bytes: 32,768 workers of 58 requests 29.1 us, 154 MB of DRAM at 0.82 of the measured copy
+// bandwidth; by the launch for single fleets, 2.1 us.
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
 {
@@ -525,8 +531,8 @@ __global__ void __launch_bounds__(256) br_slot_newest_kernel(const SlotArgs a)
 
 struct alignas(32) FourSlots { long long v[4]; };
 
-// 32 bytes in one store, so that every sector is written whole and once (two of 16 bytes wrote each sector twice, 296 us for 146
-// million tokens; 219 this way)
+// 32 bytes in one store, so that every sector is written whole and once (two of 16 bytes wrote each sector twice, 294 us for 146
+// million tokens; 219 this way, both with fewer blocks a worker than now)
 __device__ __forceinline__ void store_four(FourSlots *p, const FourSlots &s)
 {
 #ifdef BR_BOUNDS
@@ -537,8 +543,10 @@ __device__ __forceinline__ void store_four(FourSlots *p, const FourSlots &s)
 }
 
 // Any number of new tokens: four in a row a lane, which take one division and one or two entries, stored as 32 aligned bytes.
-// Bound by memory: 146 million prompt tokens 200 us, 1.17 GB at 0.90 of the measured copy bandwidth.  (Two groups of a lane at
-// once, warps that take the groups of a block in turn, and streaming stores all stay within 1 % of that.)
+// Bound by memory: 146 million prompt tokens 201 us, 1.17 GB at 0.90 of the measured copy bandwidth.  (Two groups of a lane at
+// once, warps that take the groups of a block in turn, and streaming stores all stay within 1 % of that.)  Chunks of 264 workers
+// 8.2 us, by instructions: a warp moves two groups of 128 tokens, one or two table entries a lane each, after a prologue that every
+// block of the worker repeats (469 instructions a warp in all, 0.59 of the issue slots).
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
 {
@@ -628,8 +636,9 @@ __global__ void __launch_bounds__(256) br_slot_map_kernel(const SlotArgs a)
 }
 
 // The running slots move up, their blocks follow one another: item x of the worker is entry x of its list, and rows of 32 items are
-// read and written a line at a time.  Bound by memory for long requests, 37.8 million blocks 53 us at 0.82 of the measured copy
-// bandwidth, and by instructions for short ones, 2,107 workers with runs of 33 blocks 25 us.  (A lane that takes four blocks in a
+// read and written a line at a time.  Bound by memory for long requests, 37.8 million blocks 53.5 us at 0.82 of the measured copy
+// bandwidth, and by instructions for short ones, 2,107 workers with runs of 33 blocks 24.7 us in 1.19 waves (40 registers, 48 warps an
+// SM; 248 slots need four warps, and eight take 25.0).  (A lane that takes four blocks in a
 // row: 60 us and 26.6; a run at a time: 90 and 48.)
 template <bool ONE, int SPL>
 __global__ void __launch_bounds__(256, 6) br_page_lists_kernel(const PageArgs a)
