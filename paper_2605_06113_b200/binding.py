@@ -419,6 +419,8 @@ class BlockCache:
         update's ``first`` to ``first + N`` were not written and have to hold the cache's counts already (copy them in
         ahead of such an update).  The old tensors are free again, but for graphs captured with them."""
         self._refuse((n_blocks, "n_blocks", self._slot), (n_free, "n_free", self._worker))
+        if (n_blocks.data_ptr() == self._n_blocks.data_ptr()) != (n_free.data_ptr() == self._n_free.data_ptr()):
+            raise ValueError("n_blocks and n_free go together: one of them is the cache's own and the other is not")
         self._keep(n_blocks, n_free)
 
     @classmethod

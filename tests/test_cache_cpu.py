@@ -257,3 +257,17 @@ def test_block_size_is_a_whole_number():
             BlockCache(*arrays, t)
     for t in (16, 16.0, np.int64(16), torch.tensor(16)):
         assert BlockCache(*arrays, t).block_tokens == 16
+
+
+def test_commit_takes_both_counts_or_none():
+    cache = BlockCache.empty(2, 3, 4, 16, 5, 6, device="cpu")
+    nb, nf = torch.zeros_like(cache.n_blocks), torch.zeros_like(cache.n_free)
+    own, before = (cache.n_blocks, cache.n_free), cache._packed
+    for mixed in ((nb, own[1]), (own[0], nf)):
+        with pytest.raises(ValueError, match="go together"):
+            cache.commit(*mixed)
+    assert cache._packed == before and cache.n_blocks is own[0] and cache.n_free is own[1]
+    cache.commit(*own)                                                           # what it has already
+    assert cache._packed == before
+    cache.commit(nb, nf)
+    assert cache.n_blocks is nb and cache.n_free is nf
